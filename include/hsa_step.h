@@ -66,7 +66,11 @@ typedef enum hsa_step_status {
   HSA_STEP_ERR_LAUNCH = 7     /* HIP error while enqueueing or synchronizing */
 } hsa_step_status;
 
-typedef enum hsa_step_dtype { HSA_STEP_F32 = 0, HSA_STEP_BF16 = 1 } hsa_step_dtype;
+typedef enum hsa_step_dtype {
+  HSA_STEP_F32 = 0,
+  HSA_STEP_BF16 = 1,
+  HSA_STEP_E4M3 = 2 /* 8-bit cache rows, only where an entry point has a cache_dtype */
+} hsa_step_dtype;
 
 /* How a multi-layer loop sets group membership (Appendix B). */
 typedef enum hsa_step_selection {
@@ -533,6 +537,136 @@ int hsa_stack_iteration(const hsa_stack* stack, int32_t T, int32_t iter, int32_t
                         int32_t outside_period, float sigma_i, float sigma_next,
                         const int32_t* group_budget, const int64_t* group_size, int32_t n_groups,
                         int32_t selection, int32_t* n_active_host, int32_t* refreshed_host,
+                        hipStream_t stream);
+
+/* ------------------------------------------------------------------------
+ * Sequences: caches in 8 bits or in pages, attention of several sequences.
+ *
+ * The calls above serve one sample whose queries see every cached row. These
+ * serve many sequences at once: a batch of samples with active sets of
+ * different sizes, or the prompts and the generated tokens of a text model.
+ * Grouped heads: kv_heads divides heads, and query head h reads head
+ * h / (heads / kv_heads) of the keys and values. A cache has one row of
+ * kv_heads * head_dim values per token, like the caches above; a page is
+ * page_size consecutive rows of it.
+ *
+ * cache_dtype is the dtype of the fresh rows (kept as they are) or
+ * HSA_STEP_E4M3: every row holds, per head, head_dim codes of one byte and one
+ * signed exponent e, and stands for code * 2^e. e is the smallest
+ * integer in [-117, 119] with max |x| <= 448 * 2^e over the finite values of
+ * that row and head, and the codes are x * 2^-e rounded to e4m3 (4 exponent and
+ * 3 fraction bits, greatest value 448) to nearest, ties to even,
+ * saturating; values that are not finite become the NaN code. The exponent
+ * is a power of two, so it costs no accuracy of its own: a value read back
+ * is within half a step of the code, 2^-4 of itself, or within 2^(e-10) where
+ * that is more, and is exact in bf16.
+ *
+ * Row indices and page numbers outside the cache are skipped, never followed.
+ * head_dim is 64 or 128, heads * head_dim at most 2^22. Row strides are in
+ * elements, at least the row's width and at most 2^22; rows of bf16 inputs are
+ * 16-byte aligned (stride a multiple of 8), rows of fp32 inputs 4-byte.
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Fresh keys and values into cache rows, quantized as they are written for
+ * HSA_STEP_E4M3. For j < n with t = idx[j]:
+ *   k_cache[t] = k[j], v_cache[t] = v[j]
+ * Rows not in idx are not written; an index outside [0, n_rows) (-1 for a
+ * padded position) skips its row. n * kv_heads * head_dim < 2^34.
+ *   k, v             [n, kv_heads * head_dim] dtype, rows k_stride and
+ *                    v_stride elements apart (slices of one projection's output)
+ *   idx              int32 [n], duplicate-free apart from skipped entries
+ *   k_cache, v_cache [n_rows, kv_heads * head_dim] cache_dtype, 16-byte aligned
+ *                    (fp32: 4)
+ *   k_exp, v_exp     int8 [n_rows, kv_heads], HSA_STEP_E4M3 only (else ignored)
+ * The caches must not overlap the inputs, idx, the exponents or each other.
+ */
+int hsa_cache_store(int dtype, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                    const int32_t* idx, int32_t n, int64_t n_rows, int32_t kv_heads,
+                    int32_t head_dim, int cache_dtype, void* k_cache, void* v_cache,
+                    int8_t* k_exp, int8_t* v_exp, hipStream_t stream);
+
+/*
+ * Cache rows read back: k[j] = k_cache[idx[j]], v[j] = v_cache[idx[j]] for
+ * j < n, in dtype (exact: the codes' values for HSA_STEP_E4M3, a copy
+ * otherwise). An index may come twice; one outside [0, n_rows) gives a row of
+ * zeros. Arguments as for hsa_cache_store; k and v must not overlap the caches,
+ * the exponents, idx or each other (rows between the strides are left as they
+ * were, and k and v may interleave only if their spans do not overlap).
+ */
+int hsa_cache_load(int cache_dtype, const void* k_cache, const void* v_cache, const int8_t* k_exp,
+                   const int8_t* v_exp, const int32_t* idx, int32_t n, int64_t n_rows,
+                   int32_t kv_heads, int32_t head_dim, int dtype, void* k, int64_t k_stride,
+                   void* v, int64_t v_stride, hipStream_t stream);
+
+/*
+ * Attention of packed sequences of different lengths. Sequence s has the query
+ * rows cu_q[s] .. cu_q[s+1]-1 and the key/value rows cu_kv[s] .. cu_kv[s+1]-1;
+ * with L_q and L_k their counts, query i (0 <= i < L_q) sees the keys
+ *   j < L_k                    causal == 0
+ *   j <= i + L_k - L_q         causal != 0 (the last query sees every key)
+ * and only those: nothing in another row (NaN included) reaches its result.
+ *   o[i, h]   = sum_j softmax_j(scale <q[i, h], k[j, h / G]>) v[j, h / G]
+ *   lse[i, h] = log sum_j exp(scale <q[i, h], k[j, h / G]>)
+ * A query that sees no key, or only keys whose score is -infinity, has o = 0
+ * and lse = -infinity.
+ *   q           [n_q, heads * head_dim] dtype, rows q_stride elements apart
+ *   k, v        [n_kv, kv_heads * head_dim] dtype, rows k_stride, v_stride apart
+ *   cu_q, cu_kv int32 [n_seqs + 1] on the device, ascending, in [0, n_q] and
+ *               [0, n_kv] (clamped to that; for other orders the result is
+ *               unspecified). Rows of o and lse outside every sequence are left
+ *               as they were.
+ *   o           [n_q, heads * head_dim] dtype, contiguous
+ *   lse         NULL or [n_q, heads] fp32
+ *   scale       > 0, finite
+ * n_q * heads / 16 + (n_seqs + 8) * kv_heads < 2^23. o and lse must not overlap an input or
+ * each other.
+ */
+int hsa_packed_attention(int dtype, const void* q, int64_t q_stride, const void* k,
+                         int64_t k_stride, const void* v, int64_t v_stride, const int32_t* cu_q,
+                         const int32_t* cu_kv, int32_t n_seqs, int64_t n_q, int64_t n_kv,
+                         int32_t heads, int32_t kv_heads, int32_t head_dim, float scale,
+                         int32_t causal, void* o, float* lse, hipStream_t stream);
+
+/* A workspace of this size serves every call of hsa_paged_attention: 32 MiB. */
+#define HSA_STEP_PAGED_WORKSPACE_BYTES (32u << 20)
+
+/* Workspace bytes hsa_paged_attention needs, at most
+ * HSA_STEP_PAGED_WORKSPACE_BYTES. 0 where it needs none, and for invalid sizes. */
+size_t hsa_paged_attention_workspace_bytes(int dtype, int32_t n_seqs, int32_t heads,
+                                           int32_t kv_heads, int32_t head_dim, int64_t max_len);
+
+/*
+ * Attention of one new token per sequence over a paged cache. Row t of
+ * sequence s (0 <= t < kv_lens[s]) is row
+ *   page_table[s][t / page_size] * page_size + t % page_size
+ * of the caches, and
+ *   o[s, h]   = sum_t softmax_t(scale <q[s, h], k[t, h / G]>) v[t, h / G]
+ *   lse[s, h] = log sum_t exp(scale <q[s, h], k[t, h / G]>)
+ * The cached rows are split over the workgroups whatever the lengths, and
+ * the parts joined by a second kernel (an exact rearrangement of the softmax
+ * sum). A sequence of length 0 has o = 0 and lse = -infinity. Rows in a page
+ * outside [0, n_pages) are left out of the sums; page table entries past a
+ * sequence's length are not read.
+ *   q            [n_seqs, heads * head_dim] dtype, rows q_stride elements apart
+ *   k_cache, ... as for hsa_cache_store, with n_pages * page_size rows
+ *   page_table   int32 [n_seqs, max_pages]; pages may be shared by sequences
+ *   kv_lens      int32 [n_seqs] on the device, clamped to [0, max_pages * page_size]
+ *   o            [n_seqs, heads * head_dim] dtype, contiguous
+ *   lse          NULL or [n_seqs, heads] fp32
+ *   workspace    device scratch of hsa_paged_attention_workspace_bytes(dtype,
+ *                n_seqs, heads, kv_heads, head_dim, max_pages * page_size)
+ *                bytes, 16-byte aligned, overwritten; NULL where that is 0. Calls
+ *                that may overlap in time need one each; nothing in it has to start at zero.
+ * page_size >= 1; n_pages * page_size and max_pages * page_size < 2^31, n_seqs * heads < 2^24.
+ * o and lse must not overlap an input, the workspace or each other.
+ */
+int hsa_paged_attention(int dtype, const void* q, int64_t q_stride, int cache_dtype,
+                        const void* k_cache, const void* v_cache, const int8_t* k_exp,
+                        const int8_t* v_exp, const int32_t* page_table, int32_t max_pages,
+                        const int32_t* kv_lens, int32_t n_seqs, int32_t n_pages,
+                        int32_t page_size, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                        float scale, void* o, float* lse, void* workspace, size_t workspace_bytes,
                         hipStream_t stream);
 
 #ifdef __cplusplus

@@ -18,6 +18,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhsa_ste
 
 F32 = 0
 BF16 = 1
+E4M3 = 2  # 8-bit cache rows
 
 _STATUS = {
     0: "HSA_STEP_OK",
@@ -74,6 +75,15 @@ def lib() -> ctypes.CDLL:
             "hsa_assign_budgets_by_key": (ctypes.c_int, [P, I64, I32, P, P, I32, P, P]),
             "hsa_assign_budgets_workspace_bytes": (S, [I64]),
             "hsa_assign_budgets": (ctypes.c_int, [P, I64, I32, I32, P, P, I32, P, P, S, P]),
+            "hsa_cache_store": (ctypes.c_int, [ctypes.c_int, P, I64, P, I64, P, I32, I64, I32, I32, ctypes.c_int, P, P,
+                                               P, P, P]),
+            "hsa_cache_load": (ctypes.c_int, [ctypes.c_int, P, P, P, P, P, I32, I64, I32, I32, ctypes.c_int, P, I64, P,
+                                              I64, P]),
+            "hsa_packed_attention": (ctypes.c_int, [ctypes.c_int, P, I64, P, I64, P, I64, P, P, I32, I64, I64, I32, I32,
+                                                    I32, F, I32, P, P, P]),
+            "hsa_paged_attention_workspace_bytes": (S, [ctypes.c_int, I32, I32, I32, I32, I64]),
+            "hsa_paged_attention": (ctypes.c_int, [ctypes.c_int, P, I64, ctypes.c_int, P, P, P, P, P, I32, P, I32, I32,
+                                                   I32, I32, I32, I32, F, P, P, P, S, P]),
             "hsa_stack_iteration": (ctypes.c_int, [ctypes.POINTER(HsaStack), I32, I32, I32, I32, F, F, P, P,
                                                    I32, I32, P, P, P]),
         }
@@ -110,8 +120,15 @@ EXPORTED = (
     "hsa_rope_table",
     "hsa_reorder_plan",
     "hsa_permute_rows",
+    "hsa_cache_store",
+    "hsa_cache_load",
+    "hsa_packed_attention",
+    "hsa_paged_attention_workspace_bytes",
+    "hsa_paged_attention",
     "hsa_stack_iteration",
 )
+
+PAGED_WORKSPACE_BYTES = 32 << 20  # serves every call of hsa_paged_attention
 
 SELECT_VELOCITY_NORM = 0
 SELECT_L1_REL = 1
@@ -407,6 +424,150 @@ def hsa_rope_table(theta: float, head_dim: int, grid) -> torch.Tensor:
     out = torch.empty(n, dtype=torch.float32)
     _check("hsa_rope_table", lib().hsa_rope_table(theta, head_dim, *grid, ctypes.c_void_p(out.data_ptr())))
     return out.view(-1, head_dim)
+
+
+# Calls over several sequences. Their row inputs may be strided (slices of one projection's
+# output), and every tensor has to be on the current device.
+
+
+def _rows(*ts) -> None:
+    for t in ts:
+        if not t.is_cuda or t.dim() != 2 or t.stride(1) != 1:
+            raise ValueError("rows must be 2-dimensional device tensors with contiguous rows")
+
+
+def _row_stride(t) -> int:
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _here(*ts) -> None:
+    dev = torch.cuda.current_device()
+    for t in ts:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors must be on the current device (cuda:{dev}), got {t.device}")
+
+
+def _int32(*ts) -> None:
+    for t in ts:
+        if t.dtype != torch.int32:
+            raise TypeError("indices, offsets, pages and lengths are int32")
+
+
+def _head_dim(width: int, heads: int) -> int:
+    if heads < 1 or width % heads:
+        raise ValueError(f"rows of {width} values do not hold {heads} heads")
+    return width // heads
+
+
+def _cache_dtype(dt: int, k_cache, v_cache, k_exp, v_exp, kv_heads: int) -> int:
+    """Its dtype code, with the caches' and exponents' shapes and types checked."""
+    if k_cache.dtype != v_cache.dtype or k_cache.shape != v_cache.shape or k_cache.dim() != 2:
+        raise TypeError("k_cache and v_cache must match: [n_rows, kv_heads * head_dim]")
+    if k_cache.dtype != torch.float8_e4m3fn:
+        if _DTYPES.get(k_cache.dtype) != dt:
+            raise TypeError(f"caches hold the rows' dtype or float8_e4m3fn, got {k_cache.dtype}")
+        return dt
+    for e in (k_exp, v_exp):
+        if e is None or e.dtype != torch.int8 or e.shape != (k_cache.shape[0], kv_heads):
+            raise TypeError("float8_e4m3fn caches need int8 exponents [n_rows, kv_heads]")
+    return E4M3
+
+
+def hsa_cache_store(k, v, idx, n: int, kv_heads: int, k_cache, v_cache, k_exp=None, v_exp=None, stream=None) -> None:
+    """k_cache[idx[:n]] = k[:n] and the same for v, quantized on the way into
+    float8_e4m3fn caches (k_exp, v_exp: their int8 exponents [n_rows, kv_heads]);
+    an index outside the cache skips its row."""
+    _rows(k, v)
+    _dev(idx, k_cache, v_cache, k_exp, v_exp)
+    _here(k, v, idx, k_cache, v_cache, k_exp, v_exp)
+    _int32(idx)
+    dt = _dtype(k, v)
+    cd = _cache_dtype(dt, k_cache, v_cache, k_exp, v_exp, kv_heads)
+    n_rows, d = k_cache.shape
+    if k.shape[1] != d or v.shape[1] != d or n > min(k.shape[0], v.shape[0], idx.numel()):
+        raise ValueError("k and v must hold n rows of the caches' width, idx n indices")
+    st = lib().hsa_cache_store(dt, _ptr(k), _row_stride(k), _ptr(v), _row_stride(v), _ptr(idx), n, n_rows, kv_heads,
+                               _head_dim(d, kv_heads), cd, _ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp),
+                               _stream(stream))
+    _check("hsa_cache_store", st)
+
+
+def hsa_cache_load(k_cache, v_cache, idx, n: int, kv_heads: int, k, v, k_exp=None, v_exp=None, stream=None) -> None:
+    """k[:n] = k_cache[idx[:n]] and the same for v, as values of k's dtype;
+    zeros for an index outside the cache."""
+    _rows(k, v)
+    _dev(idx, k_cache, v_cache, k_exp, v_exp)
+    _here(k, v, idx, k_cache, v_cache, k_exp, v_exp)
+    _int32(idx)
+    dt = _dtype(k, v)
+    cd = _cache_dtype(dt, k_cache, v_cache, k_exp, v_exp, kv_heads)
+    n_rows, d = k_cache.shape
+    if k.shape[1] != d or v.shape[1] != d or n > min(k.shape[0], v.shape[0], idx.numel()):
+        raise ValueError("k and v must hold n rows of the caches' width, idx n indices")
+    st = lib().hsa_cache_load(cd, _ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp), _ptr(idx), n, n_rows,
+                              kv_heads, _head_dim(d, kv_heads), dt, _ptr(k), _row_stride(k), _ptr(v), _row_stride(v),
+                              _stream(stream))
+    _check("hsa_cache_load", st)
+
+
+def hsa_packed_attention(q, k, v, cu_q, cu_kv, heads: int, kv_heads: int, head_dim: int, scale: float, causal: bool,
+                         o, lse=None, stream=None) -> None:
+    """Attention of the sequences q[cu_q[s]:cu_q[s+1]] to k, v[cu_kv[s]:cu_kv[s+1]],
+    bottom-right aligned where causal; o and lse (log of the softmax sums,
+    fp32 [n_q, heads]) outside every sequence are left as they were."""
+    _rows(q, k, v)
+    _dev(cu_q, cu_kv, o, lse)
+    _here(q, k, v, cu_q, cu_kv, o, lse)
+    _int32(cu_q, cu_kv)
+    dt = _dtype(q, k, v, o)
+    n_q, n_kv, n_seqs = q.shape[0], k.shape[0], cu_q.numel() - 1
+    if cu_kv.numel() != n_seqs + 1 or n_seqs < 0:
+        raise ValueError("cu_q and cu_kv hold n_seqs + 1 offsets each")
+    if q.shape[1] != heads * head_dim or o.shape != q.shape or k.shape[1] != kv_heads * head_dim or v.shape != k.shape:
+        raise ValueError("q and o are [n_q, heads * head_dim], k and v [n_kv, kv_heads * head_dim]")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (n_q, heads)):
+        raise TypeError("lse is fp32 [n_q, heads]")
+    st = lib().hsa_packed_attention(dt, _ptr(q), _row_stride(q), _ptr(k), _row_stride(k), _ptr(v), _row_stride(v),
+                                    _ptr(cu_q), _ptr(cu_kv), n_seqs, n_q, n_kv, heads, kv_heads, head_dim, scale,
+                                    int(bool(causal)), _ptr(o), _ptr(lse), _stream(stream))
+    _check("hsa_packed_attention", st)
+
+
+def hsa_paged_attention_workspace_bytes(dtype: torch.dtype, n_seqs: int, heads: int, kv_heads: int, head_dim: int,
+                                        max_len: int) -> int:
+    return int(lib().hsa_paged_attention_workspace_bytes(_dtype(torch.empty(0, dtype=dtype)), n_seqs, heads, kv_heads,
+                                                          head_dim, max_len))
+
+
+def hsa_paged_attention(q, k_cache, v_cache, page_table, kv_lens, page_size: int, heads: int, kv_heads: int,
+                        head_dim: int, scale: float, o, workspace, k_exp=None, v_exp=None, lse=None,
+                        stream=None) -> None:
+    """One new token per sequence against its pages: row t of sequence s is row
+    page_table[s, t // page_size] * page_size + t % page_size of the caches, for
+    t < kv_lens[s]. workspace: hsa_paged_attention_workspace_bytes(q.dtype, n_seqs,
+    heads, kv_heads, head_dim, page_table.shape[1] * page_size) bytes, or
+    PAGED_WORKSPACE_BYTES for any call."""
+    _rows(q)
+    _dev(k_cache, v_cache, page_table, kv_lens, o, workspace, k_exp, v_exp, lse)
+    _here(q, k_cache, v_cache, page_table, kv_lens, o, workspace, k_exp, v_exp, lse)
+    _int32(page_table, kv_lens)
+    dt = _dtype(q, o)
+    cd = _cache_dtype(dt, k_cache, v_cache, k_exp, v_exp, kv_heads)
+    n_seqs = q.shape[0]
+    if page_size < 1:
+        raise ValueError("page_size must be at least 1")
+    if page_table.dim() != 2 or page_table.shape[0] != n_seqs or kv_lens.numel() != n_seqs:
+        raise ValueError("page_table is [n_seqs, max_pages], kv_lens [n_seqs]")
+    if q.shape[1] != heads * head_dim or o.shape != q.shape or k_cache.shape[1] != kv_heads * head_dim:
+        raise ValueError("q and o are [n_seqs, heads * head_dim], the caches [n_rows, kv_heads * head_dim]")
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (n_seqs, heads)):
+        raise TypeError("lse is fp32 [n_seqs, heads]")
+    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    st = lib().hsa_paged_attention(dt, _ptr(q), _row_stride(q), cd, _ptr(k_cache), _ptr(v_cache), _ptr(k_exp),
+                                   _ptr(v_exp), _ptr(page_table), page_table.shape[1], _ptr(kv_lens), n_seqs,
+                                   k_cache.shape[0] // page_size, page_size, heads, kv_heads, head_dim, scale,
+                                   _ptr(o), _ptr(lse), _ptr(workspace), nbytes, _stream(stream))
+    _check("hsa_paged_attention", st)
 
 
 def make_stack(*, x, v_hat, budget, w_embed, w_head, layers, caches, idx, n_active, xa, h, q, o, v_fresh,
