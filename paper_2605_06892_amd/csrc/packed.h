@@ -42,39 +42,51 @@ __device__ __forceinline__ void packed_place(const PackedGrid& g, int kv_heads, 
   tile = xcd / c + g.share * (slot - i * g.per);
 }
 
-// Tile `idx` of the batch: the sequences in order, and within a sequence the
-// last tile first (under a causal mask the longest). False past the last one.
-// Whatever the offsets hold, the rows are inside [0, n_q) and [0, n_kv).
-// Called by whole waves; the result is the same in every lane.
+// Tile `idx` of the batch: the sequences one after the other, and within a
+// sequence the last tile first (under a causal mask the longest). Up to 64 sequences
+// come in the order of their tiles, the longest first, so that what runs last is
+// short; more come as they are. False past the last tile. Whatever the offsets hold, the rows are
+// inside [0, n_q) and [0, n_kv). Called by whole waves; the result is the same in every lane.
 __device__ __forceinline__ bool find_tile(const PackedArgs& a, int idx, int rows, SeqTile& t) {
   const int lane = threadIdx.x & (kWave - 1);
   for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
     const int s = s0 + lane;
-    int q0 = 0, q1 = 0;
+    int q0 = 0, q1 = 0, k0 = 0, k1 = 0;
     if (s < a.n_seqs) {
       q0 = min(max(a.cu_q[s], 0), a.n_q);
       q1 = min(max(a.cu_q[s + 1], q0), a.n_q);
+      k0 = min(max(a.cu_kv[s], 0), a.n_kv);
+      k1 = min(max(a.cu_kv[s + 1], k0), a.n_kv);
     }
     const int tiles = (int)(((long)(q1 - q0) * a.group + rows - 1) / rows);
-    int upto = tiles;  // tiles of the sequences s0 .. s
+    int from = 0, all = 0;  // tiles before this lane's sequence, and of the 64
+    if (a.n_seqs <= kWave) {
+      for (int i = 0; i < a.n_seqs; ++i) {
+        const int n = __builtin_amdgcn_readlane(tiles, i);
+        from += n > tiles || (n == tiles && i < lane) ? n : 0;
+        all += n;
+      }
+    } else {
+      all = tiles;
 #pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const int y = __shfl_up(upto, o);
-      if (lane >= o) upto += y;
+      for (int o = 1; o < kWave; o <<= 1) {
+        const int y = __shfl_up(all, o);
+        if (lane >= o) all += y;
+      }
+      from = all - tiles;
+      all = __builtin_amdgcn_readlane(all, kWave - 1);
     }
-    const unsigned long hit = __ballot(idx < upto);
+    const unsigned long hit = __ballot(from <= idx && idx < from + tiles);
     if (hit) {
       const int l = __builtin_ctzl(hit);
       t.q0 = __builtin_amdgcn_readlane(q0, l);
       t.len_q = __builtin_amdgcn_readlane(q1, l) - t.q0;
-      const int n = __builtin_amdgcn_readlane(tiles, l);
-      t.tile = n - 1 - (idx - (__builtin_amdgcn_readlane(upto, l) - n));
-      if (t.tile < 0 || t.tile >= n) return false;  // offsets in no order
-      t.k0 = min(max(a.cu_kv[s0 + l], 0), a.n_kv);
-      t.len_k = min(max(a.cu_kv[s0 + l + 1], t.k0), a.n_kv) - t.k0;
+      t.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - (idx - __builtin_amdgcn_readlane(from, l));
+      t.k0 = __builtin_amdgcn_readlane(k0, l);
+      t.len_k = __builtin_amdgcn_readlane(k1, l) - t.k0;
       return true;
     }
-    idx -= __builtin_amdgcn_readlane(upto, kWave - 1);
+    idx -= all;
   }
   return false;
 }
@@ -84,6 +96,41 @@ __device__ __forceinline__ int keys_seen(const PackedArgs& a, const SeqTile& t, 
   return a.causal ? min(t.len_k, i + 1 + t.len_k - t.len_q) : t.len_k;
 }
 
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// true if one of 8 bf16 values is not finite
+__device__ __forceinline__ bool odd8(bf16x8 x) {
+  const u32x4 u = __builtin_bit_cast(u32x4, x);
+  unsigned r = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) r |= (u[j] & 0x7f807f80u) + 0x00800080u;
+  return r & 0x80008000u;
+}
+
+// the finite ones of 8 bf16 values, and zeros for the others
+__device__ __forceinline__ bf16x8 without_odd(bf16x8 x) {
+  u32x4 u = __builtin_bit_cast(u32x4, x);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const unsigned hit = ((u[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;  // top bit of each half that is not
+    u[j] &= ~((hit >> 15) * 0xffffu);
+  }
+  return __builtin_bit_cast(bf16x8, u);
+}
+
+// adds to 4 channels of a row the values of keys from .. end-1 that are not finite
+__device__ __forceinline__ void add_odd(f32x4& sum, const bf16* v, long stride, int from, int end) {
+  for (int n = from; n < end; ++n)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float x = (float)v[n * stride + u];
+      if ((__float_as_uint(x) & 0x7f800000u) == 0x7f800000u) sum[u] += x;
+    }
+}
+
+// bf16, 256 rows per workgroup (packed_attention_large.hip)
+hipError_t launch_packed_attention_large(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_packed_attention_f32(const PackedArgs& a, int head_dim, hipStream_t s);
 
 }  // namespace hsa

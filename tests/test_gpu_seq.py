@@ -70,6 +70,16 @@ def check(got, lse_got, want, lse_want, A, S, dtype, n_keys, dh):
 # ---------------------------------------------------------------- packed
 
 
+@pytest.fixture(params=[("bf16", ""), ("bf16", "16"), ("bf16", "32"), ("bf16", "256"), ("f32", "")],
+                ids=lambda p: p[0] + ("-rows" + p[1] if p[1] else ""))
+def form(request, monkeypatch):
+    """The dtype, with every tile of the bf16 form whatever the launch would choose."""
+    dtype, rows = request.param
+    if rows:
+        monkeypatch.setenv("HSA_PACKED_ROWS", rows)
+    return dtype
+
+
 def packed_inputs(seed, dtype, lens_q, lens_k, heads, kv, dh, lead=0, tail=0, fused=False):
     """q, k, v on the host with `lead` rows before the first sequence and `tail` after the last, and the offsets."""
     g = _gen(seed)
@@ -129,8 +139,8 @@ PACKED = [
 @pytest.mark.parametrize("lens_q,lens_k,heads,kv", PACKED, ids=lambda x: str(x).replace(" ", ""))
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("dh", [64, 128])
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_packed(dtype, dh, causal, lens_q, lens_k, heads, kv):
+def test_packed(form, dh, causal, lens_q, lens_k, heads, kv):
+    dtype = form
     q, k, v, cu_q, cu_k = packed_inputs(len(lens_q) * 100 + sum(lens_q), dtype, lens_q, lens_k, heads, kv, dh, 3, 5)
     scale = dh ** -0.5
     o, lse = Guarded(q.shape, T[dtype], 1), Guarded((q.shape[0], heads), torch.float32, 2)
@@ -146,8 +156,8 @@ def test_packed(dtype, dh, causal, lens_q, lens_k, heads, kv):
         assert torch.all(x[:3] == 7.0) and torch.all(x[rows.stop:] == 7.0)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_packed_many_sequences(dtype):
+def test_packed_many_sequences(form):
+    dtype = form
     lens = [(i * 7) % 23 for i in range(150)]
     q, k, v, cu_q, cu_k = packed_inputs(3, dtype, lens, lens, 4, 2, 64)
     o, lse = run_packed(q, k, v, cu_q, cu_k, 4, 2, 64, 0.125, True)
@@ -178,11 +188,11 @@ def test_packed_strided_rows_and_other_stream(dtype, dh):
 
 @pytest.mark.parametrize("odd", [math.inf, -math.inf, math.nan])
 @pytest.mark.parametrize("dh", [64, 128])
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("lens", [[40, 300, 20], [600, 9]])
-def test_packed_odd_values_stay_in_what_sees_them(dtype, dh, odd, lens):
+def test_packed_odd_values_stay_in_what_sees_them(form, dh, odd, lens):
     """Keys and values that are not finite reach the rows that see them and no other: the rows before them under a
     causal mask, and the neighbouring sequences, are as without them, bit for bit."""
+    dtype = form
     heads, kv, scale = 6, 2, dh ** -0.5
     q, k, v, cu, _ = packed_inputs(5, dtype, lens, lens, heads, kv, dh)
     o0, l0 = run_packed(q, k, v, cu, cu, heads, kv, dh, scale, True)
@@ -207,18 +217,18 @@ def test_packed_odd_values_stay_in_what_sees_them(dtype, dh, odd, lens):
     assert torch.equal(l0[:at + 4], l1[:at + 4]) and torch.equal(l0[cu[1]:], l1[cu[1]:])
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_packed_infinite_last_value(dtype):
+def test_packed_infinite_last_value(form):
     """The last key of a sequence whose length is no multiple of anything, with an infinite value, without a mask."""
+    dtype = form
     q, k, v, cu, _ = packed_inputs(6, dtype, [333], [333], 2, 2, 64)
     v[332, 7] = math.inf
     o, _ = run_packed(q, k, v, cu, cu, 2, 2, 64, 0.125, False)
     assert torch.all(o[:, 7] == math.inf) and torch.isfinite(o[:, :7]).all() and torch.isfinite(o[:, 8:]).all()
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_packed_large_and_infinite_scores(dtype):
+def test_packed_large_and_infinite_scores(form):
     """Scores thousands apart and of either sign, and scores of -infinity."""
+    dtype = form
     lens = [50, 400]
     q, k, v, cu, _ = packed_inputs(7, dtype, lens, lens, 4, 2, 64)
     q = q * 300
@@ -241,9 +251,9 @@ def test_packed_large_and_infinite_scores(dtype):
             check(o[a:b, c], lse[a:b, h:h + 1], want, lw[:, None], A, S, dtype, n, 64)
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-def test_packed_offsets_out_of_range_or_order(dtype):
+def test_packed_offsets_out_of_range_or_order(form):
     """Offsets past the rows are clamped to them; nothing outside the buffers is touched whatever they hold."""
+    dtype = form
     q, k, v, _, _ = packed_inputs(8, dtype, [100], [120], 4, 2, 64)
     o = Guarded(q.shape, T[dtype], 3)
     o.t.fill_(7.0)
