@@ -658,7 +658,7 @@ size_t hsa_paged_attention_workspace_bytes(int dtype, int32_t n_seqs, int32_t he
  *                n_seqs, heads, kv_heads, head_dim, max_pages * page_size)
  *                bytes, 16-byte aligned, overwritten; NULL where that is 0. Calls
  *                that may overlap in time need one each; nothing in it has to start at zero.
- * page_size >= 1; n_pages * page_size and max_pages * page_size < 2^31, n_seqs * heads < 2^24.
+ * page_size >= 1; n_pages * page_size and max_pages * page_size < 2^31, n_seqs * heads < 2^23.
  * o and lse must not overlap an input, the workspace or each other.
  */
 int hsa_paged_attention(int dtype, const void* q, int64_t q_stride, int cache_dtype,

@@ -152,7 +152,7 @@ HSA_API int hsa_packed_attention(int dtype, const void* q, int64_t q_stride, con
   if (!heads_ok(heads, kv_heads, head_dim) || n_seqs < 0 || n_seqs == INT32_MAX || n_q < 0 || n_kv < 0 ||
       n_q > kMaxRows / heads || n_kv > kMaxRows || !(scale > 0.f) || !isfinite(scale))
     return HSA_STEP_ERR_SHAPE;
-  // one launch: fewer than 2^32 threads, 512 per 16 rows
+  // one launch: fewer than 2^32 threads, 512 per 16 rows or item
   if (n_q * heads / 16 + ((int64_t)n_seqs + 8) * kv_heads >= kMaxLaunch / 512) return HSA_STEP_ERR_SHAPE;
   if (n_q == 0 || n_seqs == 0) return HSA_STEP_OK;
   if (!q || !cu_q || !cu_kv || !o || (n_kv > 0 && (!k || !v))) return HSA_STEP_ERR_NULL;
@@ -209,7 +209,7 @@ HSA_API int hsa_paged_attention(int dtype, const void* q, int64_t q_stride, int 
     return HSA_STEP_ERR_SHAPE;
   const int64_t d = (int64_t)heads * head_dim, dk = (int64_t)kv_heads * head_dim;
   const int64_t n_rows = (int64_t)n_pages * page_size;
-  if (!fits(n_rows, dk, ce) || !fits(n_seqs, max_pages, 4) || (int64_t)n_seqs * heads >= kMaxLaunch / 256)
+  if (!fits(n_rows, dk, ce) || !fits(n_seqs, max_pages, 4) || (int64_t)n_seqs * heads >= kMaxLaunch / 512)
     return HSA_STEP_ERR_SHAPE;
   if (n_seqs == 0) return HSA_STEP_OK;
   const bool e4m3 = cache_dtype == HSA_STEP_E4M3;

@@ -511,9 +511,12 @@ PAGED = [
 
 @pytest.mark.parametrize("lens,page,heads,kv", PAGED, ids=lambda x: str(x).replace(" ", ""))
 @pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("bf16", "e4m3"), ("f32", "f32"), ("f32", "e4m3")])
-def test_paged(dtype, cache, dh, lens, page, heads, kv):
-    q, k, v, held, table = paged_inputs(sum(lens) + page, dtype, cache, lens, page, heads, kv, dh)
+def test_paged(dtype, cache, wide, dh, lens, page, heads, kv):
+    """wide: page tables of over 2048 rows, whose launch deals tiles of rows to the workgroups and joins the parts."""
+    q, k, v, held, table = paged_inputs(sum(lens) + page, dtype, cache, lens, page, heads, kv, dh,
+                                        max_pages=5000 // page if wide else None)
     scale = dh ** -0.5
     n_pages = k.shape[0] // page
     o = Guarded(q.shape, T[dtype], 1)
@@ -538,10 +541,10 @@ def test_paged_many_sequences_and_one_long(dtype, cache, page):
 
 
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])
-@pytest.mark.parametrize("page", [16, 32, 48])
-def test_paged_bad_pages_are_left_out(cache, page):
+@pytest.mark.parametrize("page,max_pages", [(16, None), (32, None), (48, None), (16, 200), (64, 100)])
+def test_paged_bad_pages_are_left_out(cache, page, max_pages):
     lens = [300, 100, 64]
-    q, k, v, held, table = paged_inputs(5, "bf16", cache, lens, page, 6, 3, 128)
+    q, k, v, held, table = paged_inputs(5, "bf16", cache, lens, page, 6, 3, 128, max_pages=max_pages)
     n_pages = k.shape[0] // page
     table[0, 1], table[0, 3], table[1, 0], table[2, :] = -1, n_pages, 2 ** 31 - 1, -2 ** 31
     o, lse = run_paged(q, held, table, lens, page, 6, 3, 128, 0.1)

@@ -97,7 +97,7 @@ def test_packed_of_nothing(lib):
 
 
 PAGED = dict(dtype=BF16, q=P[0], q_stride=2048, cache_dtype=E4M3, k_cache=P[1], v_cache=P[2], k_exp=P[3], v_exp=P[4],
-             page_table=P[5], max_pages=10, kv_lens=P[6], n_seqs=3, n_pages=40, page_size=64, heads=16, kv_heads=4,
+             page_table=P[5], max_pages=100, kv_lens=P[6], n_seqs=3, n_pages=40, page_size=64, heads=16, kv_heads=4,
              head_dim=128, scale=0.1, o=P[7], lse=P[8], workspace=P[9], workspace_bytes=32 << 20)
 
 
@@ -127,8 +127,8 @@ def test_paged_of_nothing(lib):
 
 def test_paged_workspace_bytes(lib):
     f = lib.hsa_paged_attention_workspace_bytes
-    assert f(BF16, 1, 16, 2, 64, 64) == 0                   # nothing to split
-    assert 0 < f(BF16, 1, 16, 2, 64, 700) < f(BF16, 64, 16, 2, 64, 700)
+    assert f(BF16, 1, 16, 2, 64, 2048) == 0                 # too short to split
+    assert 0 < f(BF16, 1, 16, 2, 64, 7000) < f(BF16, 64, 16, 2, 64, 7000)
     for args in [(BF16, 10000, 64, 8, 128, 2 ** 31 - 1), (F32, 1, 64, 64, 128, 2 ** 31 - 1), (BF16, 2, 1, 1, 64, 300)]:
         assert f(*args) <= 32 << 20 == H.PAGED_WORKSPACE_BYTES
     for args in [(E4M3, 1, 16, 2, 64, 700), (BF16, -1, 16, 2, 64, 700), (BF16, 1, 16, 3, 64, 700),
