@@ -19,6 +19,8 @@
 // resource that ends with the sequence.
 #include "packed.h"
 
+#include <cstdlib>
+
 namespace hsa {
 namespace {
 
@@ -296,7 +298,9 @@ hipError_t launch_dh(const PackedArgs& a, hipStream_t s) {
   const PackedGrid g32 = packed_grid(a.n_q, a.n_seqs, a.kv_heads, a.group, 32);
   const int cus = compute_units();
   auto rounds = [&](const PackedGrid& g) { return (g.groups + cus - 1) / cus; };
-  return 0.57 * rounds(g16) < rounds(g32) ? launch_w<DH, 16>(a, g16, s) : launch_w<DH, 32>(a, g32, s);
+  const char* forced = getenv("HSA_PACKED_ROWS");
+  const int rows = forced ? atoi(forced) : 0.57 * rounds(g16) < rounds(g32) ? 16 : 32;
+  return rows == 16 ? launch_w<DH, 16>(a, g16, s) : launch_w<DH, 32>(a, g32, s);
 }
 
 }  // namespace

@@ -427,87 +427,105 @@ def hsa_rope_table(theta: float, head_dim: int, grid) -> torch.Tensor:
 
 
 # Calls over several sequences. Their row inputs may be strided (slices of one projection's
-# output), and every tensor has to be on the current device.
+# output), and every tensor has to be on the current device. Their kernels take a few us for a
+# small batch, so each call tests everything in one expression of plain attributes (5 us of the former
+# checks, one function each, were 2) and names what is wrong only once something is.
+
+_I32, _F8 = torch.int32, torch.float8_e4m3fn
 
 
-def _rows(*ts) -> None:
+def _here() -> int:
+    try:
+        return _device() if _device else torch.cuda.current_device()
+    except RuntimeError:  # no device at all: the tensors are what the caller hears about
+        return -2
+
+
+def _held(dev: int, *ts) -> bool:
+    """Contiguous tensors on the device."""
     for t in ts:
-        if not t.is_cuda or t.dim() != 2 or t.stride(1) != 1:
-            raise ValueError("rows must be 2-dimensional device tensors with contiguous rows")
+        if t.get_device() != dev or not t.is_contiguous():
+            return False
+    return True
 
 
-def _row_stride(t) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
-
-
-def _here(*ts) -> None:
-    dev = torch.cuda.current_device()
-    for t in ts:
+def _refuse(dev: int, rows, held, int32, width, message: str):
+    """Raise what is wrong with a call: rows (2-dimensional inputs with contiguous rows), held (contiguous tensors or
+    None), int32 (index tensors), width (a sequence of (what, is fine) pairs of types, then shapes)."""
+    for t in (*rows, *held):
+        if t is not None and not t.is_cuda:
+            raise ValueError("tensors must be device tensors")
         if t is not None and t.get_device() != dev:
             raise ValueError(f"tensors must be on the current device (cuda:{dev}), got {t.device}")
-
-
-def _int32(*ts) -> None:
-    for t in ts:
-        if t.dtype != torch.int32:
+    for t in rows:
+        if t.dim() != 2 or t.stride(1) != 1:
+            raise ValueError("rows must be 2-dimensional with contiguous values")
+    for t in held:
+        if t is not None and not t.is_contiguous():
+            raise ValueError("tensors must be contiguous")
+    for t in int32:
+        if t.dtype != _I32:
             raise TypeError("indices, offsets, pages and lengths are int32")
+    for what, fine in width:
+        if not fine:
+            raise TypeError(what)
+    raise ValueError(message)
 
 
-def _head_dim(width: int, heads: int) -> int:
-    if heads < 1 or width % heads:
-        raise ValueError(f"rows of {width} values do not hold {heads} heads")
-    return width // heads
+def _caches_fit(dt, kc, vc, ke, ve, kv_heads: int) -> bool:
+    """Caches of rows' dtype dt, or of codes with their exponents (device and layout apart)."""
+    cd, shape = kc.dtype, kc.shape
+    if cd is not vc.dtype or shape != vc.shape or len(shape) != 2:
+        return False
+    if cd is not _F8:
+        return cd is dt
+    if ke is None or ve is None or ke.dtype is not torch.int8 or ve.dtype is not torch.int8:
+        return False
+    want = (shape[0], kv_heads)
+    return ke.shape == want and ve.shape == want
 
 
-def _cache_dtype(dt: int, k_cache, v_cache, k_exp, v_exp, kv_heads: int) -> int:
-    """Its dtype code, with the caches' and exponents' shapes and types checked."""
-    if k_cache.dtype != v_cache.dtype or k_cache.shape != v_cache.shape or k_cache.dim() != 2:
-        raise TypeError("k_cache and v_cache must match: [n_rows, kv_heads * head_dim]")
-    if k_cache.dtype != torch.float8_e4m3fn:
-        if _DTYPES.get(k_cache.dtype) != dt:
-            raise TypeError(f"caches hold the rows' dtype or float8_e4m3fn, got {k_cache.dtype}")
-        return dt
-    for e in (k_exp, v_exp):
-        if e is None or e.dtype != torch.int8 or e.shape != (k_cache.shape[0], kv_heads):
-            raise TypeError("float8_e4m3fn caches need int8 exponents [n_rows, kv_heads]")
-    return E4M3
+_CACHES = "caches hold the rows' dtype, or float8_e4m3fn with int8 exponents [n_rows, kv_heads], and match each other"
+
+
+def _cache_call(name: str, k, v, idx, n: int, kv_heads: int, kc, vc, ke, ve, stream) -> None:
+    dev = _here()
+    dt, kst, vst, ksh, vsh, csh = k.dtype, k.stride(), v.stride(), k.shape, v.shape, kc.shape
+    e4m3 = kc.dtype is _F8
+    if not (len(kst) == 2 == len(vst) and kst[1] == 1 == vst[1] and dt is v.dtype and dt in _DTYPES
+            and idx.dtype is _I32 and _caches_fit(dt, kc, vc, ke, ve, kv_heads) and ksh[1] == csh[1] == vsh[1]
+            and kv_heads > 0 and csh[1] % kv_heads == 0 and ksh[0] >= n <= vsh[0] and n <= idx.numel()
+            and k.get_device() == dev == v.get_device() and _held(dev, idx, kc, vc)
+            and (not e4m3 or _held(dev, ke, ve))):
+        _refuse(dev, (k, v), (idx, kc, vc, ke, ve), (idx,),
+                (("rows are bf16 or fp32, the same for k and v", dt is v.dtype and dt in _DTYPES),
+                 (_CACHES, _caches_fit(dt, kc, vc, ke, ve, kv_heads))),
+                "k and v must hold n rows of the caches' width, a multiple of kv_heads, and idx n indices")
+    dt = _DTYPES[dt]
+    rows = (k.data_ptr(), kst[0] if ksh[0] > 1 else ksh[1], v.data_ptr(), vst[0] if vsh[0] > 1 else vsh[1])
+    kep, vep = (ke.data_ptr(), ve.data_ptr()) if e4m3 else (None, None)
+    stream = _stream(stream)
+    if name == "hsa_cache_store":
+        st = lib().hsa_cache_store(dt, *rows, idx.data_ptr(), n, csh[0], kv_heads, csh[1] // kv_heads,
+                                   E4M3 if e4m3 else dt, kc.data_ptr(), vc.data_ptr(), kep, vep, stream)
+    else:
+        st = lib().hsa_cache_load(E4M3 if e4m3 else dt, kc.data_ptr(), vc.data_ptr(), kep, vep, idx.data_ptr(), n, csh[0],
+                                  kv_heads, csh[1] // kv_heads, dt, *rows, stream)
+    if st:
+        raise HsaStepError(name, st)
 
 
 def hsa_cache_store(k, v, idx, n: int, kv_heads: int, k_cache, v_cache, k_exp=None, v_exp=None, stream=None) -> None:
     """k_cache[idx[:n]] = k[:n] and the same for v, quantized on the way into
     float8_e4m3fn caches (k_exp, v_exp: their int8 exponents [n_rows, kv_heads]);
     an index outside the cache skips its row."""
-    _rows(k, v)
-    _dev(idx, k_cache, v_cache, k_exp, v_exp)
-    _here(k, v, idx, k_cache, v_cache, k_exp, v_exp)
-    _int32(idx)
-    dt = _dtype(k, v)
-    cd = _cache_dtype(dt, k_cache, v_cache, k_exp, v_exp, kv_heads)
-    n_rows, d = k_cache.shape
-    if k.shape[1] != d or v.shape[1] != d or n > min(k.shape[0], v.shape[0], idx.numel()):
-        raise ValueError("k and v must hold n rows of the caches' width, idx n indices")
-    st = lib().hsa_cache_store(dt, _ptr(k), _row_stride(k), _ptr(v), _row_stride(v), _ptr(idx), n, n_rows, kv_heads,
-                               _head_dim(d, kv_heads), cd, _ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp),
-                               _stream(stream))
-    _check("hsa_cache_store", st)
+    _cache_call("hsa_cache_store", k, v, idx, n, kv_heads, k_cache, v_cache, k_exp, v_exp, stream)
 
 
 def hsa_cache_load(k_cache, v_cache, idx, n: int, kv_heads: int, k, v, k_exp=None, v_exp=None, stream=None) -> None:
     """k[:n] = k_cache[idx[:n]] and the same for v, as values of k's dtype;
     zeros for an index outside the cache."""
-    _rows(k, v)
-    _dev(idx, k_cache, v_cache, k_exp, v_exp)
-    _here(k, v, idx, k_cache, v_cache, k_exp, v_exp)
-    _int32(idx)
-    dt = _dtype(k, v)
-    cd = _cache_dtype(dt, k_cache, v_cache, k_exp, v_exp, kv_heads)
-    n_rows, d = k_cache.shape
-    if k.shape[1] != d or v.shape[1] != d or n > min(k.shape[0], v.shape[0], idx.numel()):
-        raise ValueError("k and v must hold n rows of the caches' width, idx n indices")
-    st = lib().hsa_cache_load(cd, _ptr(k_cache), _ptr(v_cache), _ptr(k_exp), _ptr(v_exp), _ptr(idx), n, n_rows,
-                              kv_heads, _head_dim(d, kv_heads), dt, _ptr(k), _row_stride(k), _ptr(v), _row_stride(v),
-                              _stream(stream))
-    _check("hsa_cache_load", st)
+    _cache_call("hsa_cache_load", k, v, idx, n, kv_heads, k_cache, v_cache, k_exp, v_exp, stream)
 
 
 def hsa_packed_attention(q, k, v, cu_q, cu_kv, heads: int, kv_heads: int, head_dim: int, scale: float, causal: bool,
@@ -515,22 +533,28 @@ def hsa_packed_attention(q, k, v, cu_q, cu_kv, heads: int, kv_heads: int, head_d
     """Attention of the sequences q[cu_q[s]:cu_q[s+1]] to k, v[cu_kv[s]:cu_kv[s+1]],
     bottom-right aligned where causal; o and lse (log of the softmax sums,
     fp32 [n_q, heads]) outside every sequence are left as they were."""
-    _rows(q, k, v)
-    _dev(cu_q, cu_kv, o, lse)
-    _here(q, k, v, cu_q, cu_kv, o, lse)
-    _int32(cu_q, cu_kv)
-    dt = _dtype(q, k, v, o)
-    n_q, n_kv, n_seqs = q.shape[0], k.shape[0], cu_q.numel() - 1
-    if cu_kv.numel() != n_seqs + 1 or n_seqs < 0:
-        raise ValueError("cu_q and cu_kv hold n_seqs + 1 offsets each")
-    if q.shape[1] != heads * head_dim or o.shape != q.shape or k.shape[1] != kv_heads * head_dim or v.shape != k.shape:
-        raise ValueError("q and o are [n_q, heads * head_dim], k and v [n_kv, kv_heads * head_dim]")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (n_q, heads)):
-        raise TypeError("lse is fp32 [n_q, heads]")
-    st = lib().hsa_packed_attention(dt, _ptr(q), _row_stride(q), _ptr(k), _row_stride(k), _ptr(v), _row_stride(v),
-                                    _ptr(cu_q), _ptr(cu_kv), n_seqs, n_q, n_kv, heads, kv_heads, head_dim, scale,
-                                    int(bool(causal)), _ptr(o), _ptr(lse), _stream(stream))
-    _check("hsa_packed_attention", st)
+    dev = _here()
+    dt, qsh, ksh = q.dtype, q.shape, k.shape
+    qst, kst, vst = q.stride(), k.stride(), v.stride()
+    n_seqs = cu_q.numel() - 1
+    if not (len(qst) == len(kst) == len(vst) == 2 and qst[1] == kst[1] == vst[1] == 1
+            and dt is k.dtype and dt is v.dtype and dt is o.dtype and dt in _DTYPES
+            and cu_q.dtype is _I32 and cu_kv.dtype is _I32 and cu_kv.numel() == n_seqs + 1 > 0
+            and qsh[1] == heads * head_dim and o.shape == qsh and ksh[1] == kv_heads * head_dim and v.shape == ksh
+            and q.get_device() == dev == k.get_device() and v.get_device() == dev and _held(dev, cu_q, cu_kv, o)
+            and (lse is None or (lse.dtype is torch.float32 and lse.shape == (qsh[0], heads) and _held(dev, lse)))):
+        _refuse(dev, (q, k, v), (cu_q, cu_kv, o, lse), (cu_q, cu_kv),
+                (("q, k, v and o are bf16 or fp32, all the same", dt is k.dtype is v.dtype is o.dtype and dt in _DTYPES),
+                 ("lse is fp32 [n_q, heads]", lse is None or (lse.dtype is torch.float32 and lse.shape == (qsh[0], heads)))),
+                "q and o are [n_q, heads * head_dim], k and v [n_kv, kv_heads * head_dim], cu_q and cu_kv [n_seqs + 1]")
+    n_q, n_kv = qsh[0], ksh[0]
+    st = lib().hsa_packed_attention(_DTYPES[dt], q.data_ptr(), qst[0] if n_q > 1 else qsh[1], k.data_ptr(),
+                                    kst[0] if n_kv > 1 else ksh[1], v.data_ptr(), vst[0] if n_kv > 1 else ksh[1],
+                                    cu_q.data_ptr(), cu_kv.data_ptr(), n_seqs, n_q, n_kv, heads, kv_heads, head_dim, scale,
+                                    1 if causal else 0, o.data_ptr(), None if lse is None else lse.data_ptr(),
+                                    _stream(stream))
+    if st:
+        raise HsaStepError("hsa_packed_attention", st)
 
 
 def hsa_paged_attention_workspace_bytes(dtype: torch.dtype, n_seqs: int, heads: int, kv_heads: int, head_dim: int,
@@ -545,29 +569,36 @@ def hsa_paged_attention(q, k_cache, v_cache, page_table, kv_lens, page_size: int
     """One new token per sequence against its pages: row t of sequence s is row
     page_table[s, t // page_size] * page_size + t % page_size of the caches, for
     t < kv_lens[s]. workspace: hsa_paged_attention_workspace_bytes(q.dtype, n_seqs,
-    heads, kv_heads, head_dim, page_table.shape[1] * page_size) bytes, or
-    PAGED_WORKSPACE_BYTES for any call."""
-    _rows(q)
-    _dev(k_cache, v_cache, page_table, kv_lens, o, workspace, k_exp, v_exp, lse)
-    _here(q, k_cache, v_cache, page_table, kv_lens, o, workspace, k_exp, v_exp, lse)
-    _int32(page_table, kv_lens)
-    dt = _dtype(q, o)
-    cd = _cache_dtype(dt, k_cache, v_cache, k_exp, v_exp, kv_heads)
-    n_seqs = q.shape[0]
-    if page_size < 1:
-        raise ValueError("page_size must be at least 1")
-    if page_table.dim() != 2 or page_table.shape[0] != n_seqs or kv_lens.numel() != n_seqs:
-        raise ValueError("page_table is [n_seqs, max_pages], kv_lens [n_seqs]")
-    if q.shape[1] != heads * head_dim or o.shape != q.shape or k_cache.shape[1] != kv_heads * head_dim:
-        raise ValueError("q and o are [n_seqs, heads * head_dim], the caches [n_rows, kv_heads * head_dim]")
-    if lse is not None and (lse.dtype != torch.float32 or lse.shape != (n_seqs, heads)):
-        raise TypeError("lse is fp32 [n_seqs, heads]")
-    nbytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    st = lib().hsa_paged_attention(dt, _ptr(q), _row_stride(q), cd, _ptr(k_cache), _ptr(v_cache), _ptr(k_exp),
-                                   _ptr(v_exp), _ptr(page_table), page_table.shape[1], _ptr(kv_lens), n_seqs,
-                                   k_cache.shape[0] // page_size, page_size, heads, kv_heads, head_dim, scale,
-                                   _ptr(o), _ptr(lse), _ptr(workspace), nbytes, _stream(stream))
-    _check("hsa_paged_attention", st)
+    heads, kv_heads, head_dim, page_table.shape[1] * page_size) bytes (None where that is
+    0), or PAGED_WORKSPACE_BYTES for any call."""
+    dev = _here()
+    dt, qsh, qst, psh, csh = q.dtype, q.shape, q.stride(), page_table.shape, k_cache.shape
+    e4m3 = k_cache.dtype is _F8
+    if not (len(qst) == 2 and qst[1] == 1 and dt is o.dtype and dt in _DTYPES and o.shape == qsh
+            and _caches_fit(dt, k_cache, v_cache, k_exp, v_exp, kv_heads) and csh[1] == kv_heads * head_dim
+            and qsh[1] == heads * head_dim and page_table.dtype is _I32 and kv_lens.dtype is _I32
+            and len(psh) == 2 and psh[0] == qsh[0] == kv_lens.numel() and page_size > 0
+            and q.get_device() == dev and _held(dev, k_cache, v_cache, page_table, kv_lens, o)
+            and (workspace is None or _held(dev, workspace)) and (not e4m3 or _held(dev, k_exp, v_exp))
+            and (lse is None or (lse.dtype is torch.float32 and lse.shape == (qsh[0], heads) and _held(dev, lse)))):
+        _refuse(dev, (q,), (k_cache, v_cache, page_table, kv_lens, o, workspace, k_exp, v_exp, lse), (page_table, kv_lens),
+                (("q and o are bf16 or fp32, the same", dt is o.dtype and dt in _DTYPES),
+                 (_CACHES, _caches_fit(dt, k_cache, v_cache, k_exp, v_exp, kv_heads)),
+                 ("lse is fp32 [n_seqs, heads]",
+                  lse is None or (lse.dtype is torch.float32 and lse.shape == (qsh[0], heads)))),
+                "q and o are [n_seqs, heads * head_dim], the caches [n_rows, kv_heads * head_dim], page_table "
+                "[n_seqs, max_pages], kv_lens [n_seqs], page_size at least 1")
+    kep, vep = (k_exp.data_ptr(), v_exp.data_ptr()) if e4m3 else (None, None)
+    st = lib().hsa_paged_attention(_DTYPES[dt], q.data_ptr(), qst[0] if qsh[0] > 1 else qsh[1],
+                                   E4M3 if e4m3 else _DTYPES[dt], k_cache.data_ptr(), v_cache.data_ptr(), kep, vep,
+                                   page_table.data_ptr(), psh[1], kv_lens.data_ptr(), qsh[0], csh[0] // page_size,
+                                   page_size, heads, kv_heads, head_dim, scale, o.data_ptr(),
+                                   None if lse is None else lse.data_ptr(),
+                                   None if workspace is None else workspace.data_ptr(),
+                                   0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                   _stream(stream))
+    if st:
+        raise HsaStepError("hsa_paged_attention", st)
 
 
 def make_stack(*, x, v_hat, budget, w_embed, w_head, layers, caches, idx, n_active, xa, h, q, o, v_fresh,
