@@ -9,6 +9,11 @@
 
 #include "seq_common.h"
 
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+#include <cstdlib>
+
 namespace hsa {
 
 struct SeqTile {
@@ -20,26 +25,31 @@ struct SeqTile {
 // one XCD works on are those congruent to it mod c = gcd(8, kv_heads), and the
 // 8 / c XCDs of a head take its tiles in turn, so that whatever kv_heads is
 // every XCD gets as much of a causal sequence's long tiles as of its short ones, and a
-// head's keys pass through as few L2s as that allows.
+// head's keys pass through as few L2s as that allows. An XCD takes its heads
+// one after the other, or, where the keys and values of all of them fit its L2 of 4 MB, in
+// turn, tile by tile, so that every head's longest tiles come first.
 struct PackedGrid {
   int share;   // XCDs per head
   int per;     // tiles of one head on one XCD, at most
+  int heads;   // heads of an XCD
+  int turns;   // heads in turn
   int groups;  // workgroups
 };
-inline PackedGrid packed_grid(int n_q, int n_seqs, int kv_heads, int group, int rows) {
+inline PackedGrid packed_grid(const PackedArgs& a, int rows, int row_bytes) {
   int c = 8;
-  while (kv_heads % c) c >>= 1;
-  const long tiles = (long)n_q * group / rows + n_seqs;  // sum of ceil(rows of a sequence / rows of a tile), at most
-  const long share = 8 / c, per = (tiles + share - 1) / share;
-  const long groups = per * kv_heads * share;
-  return {(int)share, (int)per, groups < INT32_MAX ? (int)groups : -1};
+  while (a.kv_heads % c) c >>= 1;
+  const long tiles = (long)a.n_q * a.group / rows + a.n_seqs;  // sum of ceil(rows of a sequence / rows of a tile), at most
+  const long share = 8 / c, per = (tiles + share - 1) / share, heads = a.kv_heads / c;
+  const long groups = per * heads * 8;
+  const bool turns = heads * a.n_kv * 2 * row_bytes <= 3L << 20;
+  return {(int)share, (int)per, (int)heads, turns, groups < INT32_MAX ? (int)groups : -1};
 }
-__device__ __forceinline__ void packed_place(const PackedGrid& g, int kv_heads, int& head, int& tile) {
+__device__ __forceinline__ void packed_place(const PackedGrid& g, int& head, int& tile) {
   const int c = kXcds / g.share;
   const int xcd = blockIdx.x % kXcds, slot = blockIdx.x / kXcds;
-  const int i = slot / g.per;  // the i-th head of this XCD, all its tiles before the next head's
-  head = xcd % c + c * i;
-  tile = xcd / c + g.share * (slot - i * g.per);
+  const int n = g.turns ? g.heads : g.per, x = slot / n, y = slot - x * n;
+  head = xcd % c + c * (g.turns ? y : x);
+  tile = xcd / c + g.share * (g.turns ? x : y);
 }
 
 // Tile `idx` of the batch: the sequences one after the other, and within a
@@ -131,6 +141,41 @@ __device__ __forceinline__ void add_odd(f32x4& sum, const bf16* v, long stride, 
 
 // bf16, 256 rows per workgroup (packed_attention_large.hip)
 hipError_t launch_packed_attention_large(const PackedArgs& a, int head_dim, hipStream_t s);
+// Estimated time of a launch with tiles of `rows` rows and workgroups of `waves` waves (us,
+// MI355X), from the means of the batch's lengths, which are all the host knows: a fixed
+// part, and the tiles' share of a CU (each a start and its 32-key blocks; up to 4 tiles
+// to a CU count whole) or one tile's chain of blocks, whichever is longer.
+struct PackedCost {
+  int rows, waves;
+  double fixed, tile, block, chain;
+};
+// The cheapest of N shapes; HSA_PACKED_TILE=<rows>x<waves> forces one for measurement
+// sweeps and tests.
+template <int N>
+inline PackedCost packed_choice(const PackedArgs& a, const PackedCost (&costs)[N]) {
+  if (const char* forced = getenv("HSA_PACKED_TILE")) {
+    int rows = 0, waves = 0;
+    if (sscanf(forced, "%dx%d", &rows, &waves) == 2)
+      for (const PackedCost& c : costs)
+        if (c.rows == rows && c.waves == waves) return c;
+  }
+  const double seqs = a.n_seqs, len_q = a.n_q / seqs, len_k = a.n_kv / seqs;
+  const double blocks = std::max(0.0, len_k - (a.causal ? len_q / 2 : 0.0)) / 32;
+  const PackedCost* best = &costs[0];
+  double least = 0.0;
+  for (const PackedCost& c : costs) {
+    const double tiles = seqs * std::ceil(len_q * a.group / c.rows) * a.kv_heads;
+    const double each = tiles / compute_units();
+    const double us = c.fixed + std::max((each > 4 ? each : std::ceil(each)) * (c.tile + c.block * blocks),
+                                         c.tile + c.chain * len_k / 32);
+    if (&c == &costs[0] || us < least) {
+      best = &c;
+      least = us;
+    }
+  }
+  return *best;
+}
+
 hipError_t launch_packed_attention_f32(const PackedArgs& a, int head_dim, hipStream_t s);
 
 }  // namespace hsa

@@ -3,8 +3,8 @@
 //   o_i = sum_j softmax_j(scale <q_i, k_j>) v_j over the keys that query i sees
 //
 // Small tiles (this file): 16 or 32 rows (see packed.h) of one key/value head per
-// workgroup, whose 8 waves split the keys (wave w takes the 32-key blocks w,
-// w+8, ...) and merge their softmaxes in LDS; no wave waits for another before
+// workgroup, whose 4 or 8 waves split the keys (wave w takes the 32-key blocks w,
+// w+NW, ...) and merge their softmaxes in LDS; no wave waits for another before
 // that. Per block of a wave: S^T = K Q^T by v_mfma_f32_16x16x32_bf16 (32x32x16 for 32
 // rows), K rows straight from global memory in the A operand's layout; each lane holds
 // scores of ONE row, which are the B operand of O^T += V^T P^T as they sit. V
@@ -25,7 +25,6 @@ namespace {
 
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
-constexpr int kWaves = 8;
 constexpr int kKeys = 32;  // keys per block
 
 // The W x W bf16 matrix instruction: 64/W contraction slots (lane / W) of 8
@@ -47,9 +46,9 @@ struct MfmaB<32> {
   }
 };
 
-// W: rows per workgroup
-template <int DH, int W>
-__global__ __launch_bounds__(kWaves * 64) void packed_small_kernel(PackedArgs a, PackedGrid grid) {
+// W: rows per workgroup, NW: its waves
+template <int DH, int W, int NW>
+__global__ __launch_bounds__(NW * 64) void packed_small_kernel(PackedArgs a, PackedGrid grid) {
   typedef typename MfmaB<W>::acc Acc;
   constexpr int SL = 64 / W;               // contraction slots
   constexpr int NE = W / SL;               // result registers per lane
@@ -60,13 +59,13 @@ __global__ __launch_bounds__(kWaves * 64) void packed_small_kernel(PackedArgs a,
   constexpr int CPR = DH / 8;              // 16-byte chunks per row
   constexpr int LV = kKeys * CPR / 64;     // V loads per lane and block
   constexpr int P = DH + 4;                // padded row of the merge buffer, floats
-  __shared__ __attribute__((aligned(16))) float buf[kWaves][W * P];  // V rows, then the merge
-  __shared__ float m_part[kWaves][W], l_part[kWaves][W];
-  __shared__ int odd_part[kWaves];
+  __shared__ __attribute__((aligned(16))) float buf[NW][W * P];  // V rows, then the merge
+  __shared__ float m_part[NW][W], l_part[NW][W];
+  __shared__ int odd_part[NW];
   static_assert(W * P * 4 >= kKeys * DH * 2, "a block's V rows fit");
   int h, idx;
   SeqTile t;
-  packed_place(grid, a.kv_heads, h, idx);
+  packed_place(grid, h, idx);
   if (!find_tile(a, idx, W, t)) return;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -139,7 +138,7 @@ __global__ __launch_bounds__(kWaves * 64) void packed_small_kernel(PackedArgs a,
   // value is NaN. In blocks that some row does not see whole, values that are not
   // finite are left out of the products, and the merge adds them to the rows that see them.
   bool cut_odd = false;
-  for (int n0 = wave * kKeys; n0 < seen_hi; n0 += kWaves * kKeys) {
+  for (int n0 = wave * kKeys; n0 < seen_hi; n0 += NW * kKeys) {
     const bool cut = n0 + kKeys > seen_lo;  // some row does not see every key of the block
     if (cut) {
       bool odd = false;
@@ -164,7 +163,7 @@ __global__ __launch_bounds__(kWaves * 64) void packed_small_kernel(PackedArgs a,
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) s[kt] = MfmaB<W>::mul(kf[kt][kk], qf[kk], s[kt]);
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");  // the V rows are in LDS
-    load(n0 + kWaves * kKeys);
+    load(n0 + NW * kKeys);
     if (cut) {
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
@@ -228,18 +227,18 @@ __global__ __launch_bounds__(kWaves * 64) void packed_small_kernel(PackedArgs a,
   __syncthreads();
   bool any_odd = false;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) any_odd |= odd_part[w] != 0;
-  for (int f = threadIdx.x; f < W * DH / 4; f += kWaves * 64) {
+  for (int w = 0; w < NW; ++w) any_odd |= odd_part[w] != 0;
+  for (int f = threadIdx.x; f < W * DH / 4; f += NW * 64) {
     const int r = f / (DH / 4), c = (f - r * (DH / 4)) * 4;
     const int R = r0 + r;
     if (R >= n_rows) continue;
     float m = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, m_part[w][r]);
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, m_part[w][r]);
     f32x4 sum = {};
     float l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float mw = m_part[w][r];
       if (mw == -INFINITY && l_part[w][r] == 0.f) continue;  // no key, or no finite score
       const float wt = __builtin_amdgcn_exp2f((mw - m) * sl2e);
@@ -256,46 +255,37 @@ __global__ __launch_bounds__(kWaves * 64) void packed_small_kernel(PackedArgs a,
   }
 }
 
-template <int DH, int W>
+template <int DH, int W, int NW>
 hipError_t launch_small(const PackedArgs& a, hipStream_t s) {
-  const PackedGrid g = packed_grid(a.n_q, a.n_seqs, a.kv_heads, a.group, W);
+  const PackedGrid g = packed_grid(a, W, DH * 2);
   if (g.groups < 0) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((packed_small_kernel<DH, W>), dim3((unsigned)g.groups), dim3(kWaves * 64), 0, s, a, g);
+  hipLaunchKernelGGL((packed_small_kernel<DH, W, NW>), dim3((unsigned)g.groups), dim3(NW * 64), 0, s, a, g);
   return hipGetLastError();
 }
 
-// Estimated time of a launch with tiles of `rows` rows (us, MI355X), from the
-// means of the batch's lengths, which are all the host knows: a fixed part, and
-// the tiles' share of a CU (each a start and its 32-key blocks) or one tile's chain of
-// blocks, whichever is longer. Fitted to 499 launches of 1 to 20 prompts of 1 to 4500
-// tokens, with and without 1000 rows before them, 1 to 40 heads of either width, where the
-// least estimate takes 1.3% more than the fastest of the three on average and over 10% more in
-// one of 23. Measured at 128-wide heads, 16, 32 and 256 rows: 1 prompt of 400 tokens, 8 heads
-// 9.7, 11.1 and 16.7; of 1000 20.5, 17.7 and 30.0; of 4500 224, 137 and 100;
-// 20 prompts of 233 to 700, 8 heads 126, 84 and 36.
-struct Cost {
-  int rows;
-  double fixed, tile, block, chain;
-};
-constexpr Cost kCosts[2][3] = {
-    {{16, 2.8, 2.2, 0.136, 0.14}, {32, 0.8, 4.7, 0.20, 0.15}, {256, 0.0, 7.0, 0.78, 0.45}},   // 64-wide heads
-    {{16, 0.6, 4.9, 0.32, 0.28}, {32, 0.0, 6.5, 0.41, 0.32}, {256, 0.0, 8.4, 1.26, 0.68}}};  // 128-wide
+// Fitted to 499 launches of 1, 5 and 20 prompts of 1 to 4500 tokens, with and without 1000
+// rows before them, 1 to 40 heads of either width: the least estimate takes 1.5% more
+// than the fastest of the five on average, over 10% more in one launch of 20. Measured, 128-wide
+// heads, in this order: 8 heads, 1 prompt of 400 tokens 9.7, 10.3, 11.1, 12.0 and 16.7;
+// of 1000 20.5, 19.2, 17.7, 19.5 and 30.0; of 4500 224, 217, 137, 139 and 100;
+// 20 prompts of 25 to 77, 8 heads 14.9, 12.1, 13.2, 14.8 and 9.3.
+constexpr PackedCost kCosts[2][5] = {{{16, 8, 2.6, 2.3, 0.127, 0.141},   // 64-wide heads
+                                      {16, 4, 3.9, 0.93, 0.142, 0.05},
+                                      {32, 8, 0.0, 5.3, 0.164, 0.026},
+                                      {32, 4, 2.8, 2.6, 0.161, 0.203},
+                                      {256, 8, 0.0, 6.7, 0.513, 0.332}},
+                                     {{16, 8, 0.0, 5.4, 0.289, 0.08},    // 128-wide
+                                      {16, 4, 3.3, 2.4, 0.272, 0.125},
+                                      {32, 8, 0.0, 6.4, 0.346, 0.161},
+                                      {32, 4, 0.0, 6.9, 0.348, 0.298},
+                                      {256, 8, 0.0, 8.0, 0.78, 0.487}}};
 
-int choose_rows(const PackedArgs& a, int head_dim) {
-  const double seqs = a.n_seqs, len_q = a.n_q / seqs, len_k = a.n_kv / seqs;
-  const double blocks = std::max(0.0, len_k - (a.causal ? len_q / 2 : 0.0)) / kKeys;
-  int rows = 0;
-  double best = 0.0;
-  for (const Cost& c : kCosts[head_dim == 128]) {
-    const double tiles = seqs * std::ceil(len_q * a.group / c.rows) * a.kv_heads;
-    const double us = c.fixed + std::max(tiles * (c.tile + c.block * blocks) / compute_units(),
-                                         c.tile + c.chain * len_k / kKeys);
-    if (!rows || us < best) {
-      rows = c.rows;
-      best = us;
-    }
-  }
-  return rows;
+template <int DH>
+hipError_t launch_dh(const PackedArgs& a, hipStream_t s) {
+  const PackedCost c = packed_choice(a, kCosts[DH == 128]);
+  if (c.rows == 256) return launch_packed_attention_large(a, DH, s);
+  if (c.rows == 32) return c.waves == 8 ? launch_small<DH, 32, 8>(a, s) : launch_small<DH, 32, 4>(a, s);
+  return c.waves == 8 ? launch_small<DH, 16, 8>(a, s) : launch_small<DH, 16, 4>(a, s);
 }
 
 }  // namespace
@@ -303,12 +293,7 @@ int choose_rows(const PackedArgs& a, int head_dim) {
 hipError_t launch_packed_attention(const PackedArgs& a, bool bf16, int head_dim, hipStream_t s) {
   if (a.n_q <= 0 || a.n_seqs <= 0) return hipSuccess;
   if (!bf16) return launch_packed_attention_f32(a, head_dim, s);
-  // HSA_PACKED_ROWS=16, 32 or 256 forces a tile for measurement sweeps and tests
-  const char* forced = getenv("HSA_PACKED_ROWS");
-  const int rows = forced ? atoi(forced) : choose_rows(a, head_dim);
-  if (rows == 256) return launch_packed_attention_large(a, head_dim, s);
-  if (rows == 32) return head_dim == 64 ? launch_small<64, 32>(a, s) : launch_small<128, 32>(a, s);
-  return head_dim == 64 ? launch_small<64, 16>(a, s) : launch_small<128, 16>(a, s);
+  return head_dim == 64 ? launch_dh<64>(a, s) : launch_dh<128>(a, s);
 }
 
 }  // namespace hsa

@@ -1,14 +1,14 @@
 // fp32 attention of packed sequences with grouped heads, causal or not.
 //
-// Both contractions run on the matrix cores in fp32 (v_mfma_f32_32x32x2_f32 or
-// 16x16x4), which bound it. One workgroup of 8 waves takes 32 (or 16) rows (see packed.h)
+// Both contractions run on the matrix cores in fp32 (v_mfma_f32_16x16x4_f32),
+// which bound it. One workgroup of 4 or 8 waves takes 16 rows (see packed.h)
 // of one key/value head and its waves split the keys the tile sees (wave w
-// takes the 32-key blocks w, w+8, ...); the eight partial softmaxes are merged
-// through LDS. Per 32-key block, in one wave (32 rows; 16 are alike):
-//   S^T = K Q^T     K rows are the A operand (lane: key l%32), the queries the
+// takes the 32-key blocks w, w+NW, ...); their partial softmaxes are merged
+// through LDS. Per 32-key block, in one wave:
+//   S^T = K Q^T     K rows are the A operand (lane: key l%16), the queries the
 //                   B operand. The contraction order is free, so a lane reads
-//                   runs of 4 channels (16 bytes) and step 4j + t of slot hi
-//                   takes channel 8j + 4hi + t. Each lane then holds 16 scores
+//                   runs of 4 channels (16 bytes) and step 4j + t of slot l/16
+//                   takes channel 16j + 4 (l/16) + t. Each lane then holds 8 scores
 //                   of ONE row.
 //   softmax         online; exp_neg is as exact as expf for x <= 0.
 //   O^T += V^T P^T  step e takes the probabilities as they sit in the score
@@ -19,20 +19,18 @@
 // resource that ends with the sequence.
 #include "packed.h"
 
-#include <cstdlib>
-
 namespace hsa {
 namespace {
 
-constexpr int kWaves = 8;  // waves per workgroup, each on its own key blocks
-constexpr int kThreads = kWaves * kWave;
+constexpr int W = 16;      // rows per workgroup
 constexpr int kKeys = 32;  // keys per block
 
 __device__ __forceinline__ bool odd(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 
-// W: rows per workgroup
-template <int DH, int W>
-__global__ __launch_bounds__(kThreads) void packed_f32_kernel(PackedArgs a, PackedGrid grid) {
+// NW: waves, each on its own key blocks
+template <int DH, int NW>
+__global__ __launch_bounds__(NW * kWave, DH == 64 ? 4 : 2) void packed_f32_kernel(PackedArgs a, PackedGrid grid) {
+  constexpr int kThreads = NW * kWave;
   typedef typename Mfma<W>::acc Acc;
   constexpr int SL = kWave / W;        // contraction slots of one instruction
   constexpr int NE = W / SL;           // result registers per lane
@@ -42,18 +40,16 @@ __global__ __launch_bounds__(kThreads) void packed_f32_kernel(PackedArgs a, Pack
   constexpr int CPR = DH / 4;          // 16-byte chunks per row
   constexpr int LD = kKeys * CPR / kWave;  // 16-byte loads per lane of a block's K rows
   constexpr int P = DH + 4;            // padded LDS row, floats
-  constexpr bool kQLds = DH > 64 && W > 16;
   typedef float vrow __attribute__((ext_vector_type(DT)));
-  typedef vrow vrow_lds __attribute__((aligned(DT < 4 ? 4 * DT : 16)));
+  typedef vrow vrow_lds __attribute__((aligned(16)));
   static_assert(P * 4 % alignof(vrow_lds) == 0, "rows of the merge buffer are aligned for its stores");
   // per wave: its block's K rows, at the end its share of the output
-  __shared__ __attribute__((aligned(16))) float buf[kWaves][kKeys * P];
-  __shared__ float m_part[kWaves][W], l_part[kWaves][W];
-  __shared__ int odd_part[kWaves];
-  __shared__ __attribute__((aligned(16))) float q_lds[kQLds ? W * P : 4];
+  __shared__ __attribute__((aligned(16))) float buf[NW][kKeys * P];
+  __shared__ float m_part[NW][W], l_part[NW][W];
+  __shared__ int odd_part[NW];
   int h, idx;
   SeqTile t;
-  packed_place(grid, a.kv_heads, h, idx);
+  packed_place(grid, h, idx);
   if (!find_tile(a, idx, W, t)) return;
 
   const int lane = threadIdx.x & (kWave - 1);
@@ -66,29 +62,15 @@ __global__ __launch_bounds__(kThreads) void packed_f32_kernel(PackedArgs a, Pack
   const float* kg = static_cast<const float*>(a.k) + t.k0 * a.k_stride + (long)h * DH;
   const float* vg = static_cast<const float*>(a.v) + t.k0 * a.v_stride + (long)h * DH;
 
-  // rows past the sequence repeat its last one and are not stored
-  auto q_row = [&](int r) {
-    const int R = min(r0 + r, n_rows - 1), i = R / a.group;
-    return static_cast<const float*>(a.q) + (t.q0 + i) * a.q_stride + (long)(h * a.group + R - i * a.group) * DH;
-  };
-  // this lane's row: in registers, or where those hold the next block's K rows
-  // instead (32 rows of 128 channels) in LDS, the same for every wave
-  f32x4 qf[kQLds ? 1 : J];
-  if constexpr (kQLds) {
-    for (int f = threadIdx.x; f < W * CPR; f += kThreads) {
-      const int r = f / CPR, c = (f - r * CPR) * 4;
-      *reinterpret_cast<f32x4*>(&q_lds[r * P + c]) = *reinterpret_cast<const f32x4u*>(q_row(r) + c);
-    }
-    __syncthreads();
-  } else {
-    const float* qr = q_row(lw) + slot * 4;
+  // this lane's row (rows past the sequence repeat its last one and are not stored)
+  f32x4 qf[J];
+  {
+    const int R = min(r0 + lw, n_rows - 1), i = R / a.group;
+    const float* qr = static_cast<const float*>(a.q) + (t.q0 + i) * a.q_stride +
+                      (long)(h * a.group + R - i * a.group) * DH + slot * 4;
 #pragma unroll
     for (int j = 0; j < J; ++j) qf[j] = *reinterpret_cast<const f32x4u*>(qr + j * 4 * SL);
   }
-  auto query = [&](int j) -> f32x4 {
-    if constexpr (kQLds) return *reinterpret_cast<const f32x4*>(&q_lds[lw * P + j * 4 * SL + slot * 4]);
-    else return qf[j];
-  };
 
   // Maxima are of the products q.k and the scale follows the subtraction: the
   // exponents (q.k - m) scale are at most 0 however large the products are.
@@ -114,15 +96,10 @@ __global__ __launch_bounds__(kThreads) void packed_f32_kernel(PackedArgs a, Pack
       vo += so;
       so = 0;
     }
-    if constexpr (C == 2) {
-      const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(rs, vo, so, 0);
-      __builtin_memcpy(dst, &x, sizeof(x));
-    } else {
 #pragma unroll
-      for (int i = 0; i < C / 4; ++i) {
-        const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rs, vo + i * 16, so, 0);
-        __builtin_memcpy(reinterpret_cast<char*>(dst) + i * 16, &x, sizeof(x));
-      }
+    for (int i = 0; i < C / 4; ++i) {
+      const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rs, vo + i * 16, so, 0);
+      __builtin_memcpy(reinterpret_cast<char*>(dst) + i * 16, &x, sizeof(x));
     }
   };
 
@@ -146,7 +123,7 @@ __global__ __launch_bounds__(kThreads) void packed_f32_kernel(PackedArgs a, Pack
         read(&vf[kt][e], vg, (int)a.v_stride, n0, Mfma<W>::row(0, slot), kt * W + Mfma<W>::row(e, 0), lw * DT);
   };
   load_k(wave * kKeys);
-  for (int n0 = wave * kKeys; n0 < seen_hi; n0 += kWaves * kKeys) {
+  for (int n0 = wave * kKeys; n0 < seen_hi; n0 += NW * kKeys) {
     const bool cut = n0 + kKeys > seen_lo;  // some row does not see every key of the block
 #pragma unroll
     for (int i = 0; i < LD; ++i) {
@@ -160,17 +137,15 @@ __global__ __launch_bounds__(kThreads) void packed_f32_kernel(PackedArgs a, Pack
     for (int kt = 0; kt < KT; ++kt) s[kt] = (Acc){};
 #pragma unroll
     for (int j = 0; j < J; ++j) {
-      if (kQLds && j % 4 == 0) __builtin_amdgcn_sched_barrier(0);  // else every LDS read is hoisted, and spills
-      const f32x4 qv = query(j);
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) {
         const f32x4 kf = *reinterpret_cast<const f32x4*>(&kl[(kt * W + lw) * P + j * 4 * SL + slot * 4]);
 #pragma unroll
-        for (int u = 0; u < 4; ++u) s[kt] = Mfma<W>::mul(kf[u], qv[u], s[kt]);
+        for (int u = 0; u < 4; ++u) s[kt] = Mfma<W>::mul(kf[u], qf[j][u], s[kt]);
       }
     }
     __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");  // read before the next block's rows
-    load_k(n0 + kWaves * kKeys);
+    load_k(n0 + NW * kKeys);
 
     if (cut) {
       bool odd_v = false;
@@ -245,18 +220,18 @@ __global__ __launch_bounds__(kThreads) void packed_f32_kernel(PackedArgs a, Pack
   __syncthreads();
   bool any_odd = false;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) any_odd |= odd_part[w] != 0;
+  for (int w = 0; w < NW; ++w) any_odd |= odd_part[w] != 0;
   for (int f = threadIdx.x; f < W * CPR; f += kThreads) {
     const int r = f / CPR, c = (f - r * CPR) * 4;
     const int R = r0 + r;
     if (R >= n_rows) continue;
     float m = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) m = fmaxf(m, m_part[w][r]);
+    for (int w = 0; w < NW; ++w) m = fmaxf(m, m_part[w][r]);
     f32x4 sum = {};
     float l = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < NW; ++w) {
       const float mw = m_part[w][r];
       if (mw == -INFINITY && l_part[w][r] == 0.f) continue;  // no key, or no finite score
       const float wt = expf((mw - m) * a.scale);
@@ -282,25 +257,26 @@ __global__ __launch_bounds__(kThreads) void packed_f32_kernel(PackedArgs a, Pack
   }
 }
 
-template <int DH, int W>
-hipError_t launch_w(const PackedArgs& a, const PackedGrid& g, hipStream_t s) {
+template <int DH, int NW>
+hipError_t launch_waves(const PackedArgs& a, hipStream_t s) {
+  const PackedGrid g = packed_grid(a, W, DH * 4);
   if (g.groups < 0) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((packed_f32_kernel<DH, W>), dim3((unsigned)g.groups), dim3(kThreads), 0, s, a, g);
+  hipLaunchKernelGGL((packed_f32_kernel<DH, NW>), dim3((unsigned)g.groups), dim3(NW * kWave), 0, s, a, g);
   return hipGetLastError();
 }
 
+// 8 waves where few tiles leave a CU to each, 4 where the CUs share many: fitted to
+// 444 launches like the bf16 form's tiles (see there), where the lesser estimate takes
+// 1.3% more than the faster of the two on average. Measured with 64-wide heads, 4 and 8
+// waves: 1 prompt of 1000 tokens, 1 head 19.1 and 17.1; 5 prompts of 33 to 700, 12 heads
+// 34.7 and 38.9. (32 rows per workgroup, 8 waves: 27.7 and 47.7.)
+constexpr PackedCost kCosts[2][2] = {{{W, 8, 3.6, 3.2, 0.329, 0.062}, {W, 4, 5.6, 1.25, 0.362, 0.115}},  // 64-wide heads
+                                     {{W, 8, 0.0, 8.3, 0.697, 0.27}, {W, 4, 3.6, 4.6, 0.672, 0.804}}};  // 128-wide
+
 template <int DH>
 hipError_t launch_dh(const PackedArgs& a, hipStream_t s) {
-  // 32 rows per workgroup, or 16 where that fills the CUs better: a round of
-  // 16-row workgroups takes 0.57 of a round of 32-row ones (each wave loads
-  // the same keys for half the products)
-  const PackedGrid g16 = packed_grid(a.n_q, a.n_seqs, a.kv_heads, a.group, 16);
-  const PackedGrid g32 = packed_grid(a.n_q, a.n_seqs, a.kv_heads, a.group, 32);
-  const int cus = compute_units();
-  auto rounds = [&](const PackedGrid& g) { return (g.groups + cus - 1) / cus; };
-  const char* forced = getenv("HSA_PACKED_ROWS");
-  const int rows = forced ? atoi(forced) : 0.57 * rounds(g16) < rounds(g32) ? 16 : 32;
-  return rows == 16 ? launch_w<DH, 16>(a, g16, s) : launch_w<DH, 32>(a, g32, s);
+  const PackedCost c = packed_choice(a, kCosts[DH == 128]);
+  return c.waves == 4 ? launch_waves<DH, 4>(a, s) : launch_waves<DH, 8>(a, s);
 }
 
 }  // namespace

@@ -72,7 +72,7 @@ __global__ __launch_bounds__(NW * 64) void packed_large_kernel(PackedArgs a, Pac
   __shared__ int odd_flag;  // a value was taken out, see take_odd
   int h, idx;
   SeqTile t;
-  packed_place(grid, a.kv_heads, h, idx);
+  packed_place(grid, h, idx);
   if (!find_tile(a, idx, BQ, t)) return;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // uniform: scalar
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(NW * 64) void packed_large_kernel(PackedArgs a, Pac
 
 template <int DH>
 hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  const PackedGrid g = packed_grid(a.n_q, a.n_seqs, a.kv_heads, a.group, BQ);
+  const PackedGrid g = packed_grid(a, BQ, DH * 2);
   if (g.groups < 0) return hipErrorInvalidValue;
   hipLaunchKernelGGL((packed_large_kernel<DH>), dim3((unsigned)g.groups), dim3(NW * 64), 0, s, a, g);
   return hipGetLastError();

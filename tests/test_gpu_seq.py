@@ -70,13 +70,14 @@ def check(got, lse_got, want, lse_want, A, S, dtype, n_keys, dh):
 # ---------------------------------------------------------------- packed
 
 
-@pytest.fixture(params=[("bf16", ""), ("bf16", "16"), ("bf16", "32"), ("bf16", "256"), ("f32", "")],
-                ids=lambda p: p[0] + ("-rows" + p[1] if p[1] else ""))
+@pytest.fixture(params=[("bf16", ""), ("bf16", "16x8"), ("bf16", "16x4"), ("bf16", "32x8"), ("bf16", "32x4"),
+                        ("bf16", "256x8"), ("f32", "16x8"), ("f32", "16x4")],
+                ids=lambda p: "-".join(filter(None, p)))
 def form(request, monkeypatch):
-    """The dtype, with every tile of the bf16 form whatever the launch would choose."""
-    dtype, rows = request.param
-    if rows:
-        monkeypatch.setenv("HSA_PACKED_ROWS", rows)
+    """The dtype, with every tile (rows x waves) whatever the launch would choose."""
+    dtype, tile = request.param
+    if tile:
+        monkeypatch.setenv("HSA_PACKED_TILE", tile)
     return dtype
 
 
