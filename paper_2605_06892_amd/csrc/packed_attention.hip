@@ -76,9 +76,9 @@ __global__ __launch_bounds__(NW * 64) void packed_small_kernel(PackedArgs a, Pac
   // this lane's row (rows past the sequence repeat its last one and are not stored)
   const int n_rows = t.len_q * a.group, r0 = t.tile * W;
   const int row = min(r0 + lw, n_rows - 1);
-  const int seen = keys_seen(a, t, row / a.group);
-  const int seen_lo = keys_seen(a, t, r0 / a.group);  // the least and the greatest of the tile
-  const int seen_hi = keys_seen(a, t, min(r0 + W - 1, n_rows - 1) / a.group);
+  const int seen = keys_seen(a, t, (int)a.by_group.quot(row));
+  const int seen_lo = keys_seen(a, t, (int)a.by_group.quot(r0));  // the least and the greatest of the tile
+  const int seen_hi = keys_seen(a, t, (int)a.by_group.quot(min(r0 + W - 1, n_rows - 1)));
 
   const bf16* kg = static_cast<const bf16*>(a.k) + (long)t.k0 * a.k_stride + (long)h * DH;
   const bf16* vg = static_cast<const bf16*>(a.v) + (long)t.k0 * a.v_stride + (long)h * DH;
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(NW * 64) void packed_small_kernel(PackedArgs a, Pac
 
   bf16x8 qf[KK];
   {
-    const int i = row / a.group;
+    const int i = (int)a.by_group.quot(row);
     const bf16* qr = static_cast<const bf16*>(a.q) + (t.q0 + i) * a.q_stride +
                      (long)(h * a.group + row - i * a.group) * DH + slot * 8;
 #pragma unroll
@@ -245,7 +245,7 @@ __global__ __launch_bounds__(NW * 64) void packed_small_kernel(PackedArgs a, Pac
       l = fmaf(wt, l_part[w][r], l);
       sum += wt * *reinterpret_cast<const f32x4*>(&buf[w][r * P + c]);
     }
-    const int i = R / a.group, hq = h * a.group + R - i * a.group;
+    const int i = (int)a.by_group.quot(R), hq = h * a.group + R - i * a.group;
     const long orow = (long)(t.q0 + i) * (a.kv_heads * a.group) + hq;
     sum *= l == 0.f ? 0.f : 1.f / l;
     if (any_odd) add_odd(sum, vg + c, a.v_stride, max(seen_lo, 0) / kKeys * kKeys, keys_seen(a, t, i));

@@ -56,16 +56,16 @@ __global__ __launch_bounds__(NW * kWave, DH == 64 ? 4 : 2) void packed_f32_kerne
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int lw = lane % W, slot = lane / W;
   const int n_rows = t.len_q * a.group, r0 = t.tile * W;
-  const int seen = keys_seen(a, t, min(r0 + lw, n_rows - 1) / a.group);
-  const int seen_lo = keys_seen(a, t, r0 / a.group);
-  const int seen_hi = keys_seen(a, t, min(r0 + W - 1, n_rows - 1) / a.group);
+  const int seen = keys_seen(a, t, (int)a.by_group.quot(min(r0 + lw, n_rows - 1)));
+  const int seen_lo = keys_seen(a, t, (int)a.by_group.quot(r0));
+  const int seen_hi = keys_seen(a, t, (int)a.by_group.quot(min(r0 + W - 1, n_rows - 1)));
   const float* kg = static_cast<const float*>(a.k) + t.k0 * a.k_stride + (long)h * DH;
   const float* vg = static_cast<const float*>(a.v) + t.k0 * a.v_stride + (long)h * DH;
 
   // this lane's row (rows past the sequence repeat its last one and are not stored)
   f32x4 qf[J];
   {
-    const int R = min(r0 + lw, n_rows - 1), i = R / a.group;
+    const int R = min(r0 + lw, n_rows - 1), i = (int)a.by_group.quot(R);
     const float* qr = static_cast<const float*>(a.q) + (t.q0 + i) * a.q_stride +
                       (long)(h * a.group + R - i * a.group) * DH + slot * 4;
 #pragma unroll
@@ -241,7 +241,7 @@ __global__ __launch_bounds__(NW * kWave, DH == 64 ? 4 : 2) void packed_f32_kerne
       for (int u = 0; u < 4; ++u) sum[u] = fmaf(wt, x[u], sum[u]);
     }
     sum *= l == 0.f ? 0.f : 1.f / l;
-    const int i = R / a.group, hq = h * a.group + R - i * a.group;
+    const int i = (int)a.by_group.quot(R), hq = h * a.group + R - i * a.group;
     const long orow = (long)(t.q0 + i) * (a.kv_heads * a.group) + hq;
     if (any_odd) {
       const int end = keys_seen(a, t, i);

@@ -81,21 +81,28 @@ __global__ __launch_bounds__(NW * 64) void packed_large_kernel(PackedArgs a, Pac
 
   // this lane's row (rows past the sequence repeat its last one and are not stored)
   const int n_rows = t.len_q * a.group, r0 = t.tile * BQ, rw = r0 + wave * 32;
-  const int row = min(rw + l32, n_rows - 1), qi = row / a.group;
+  const int row = min(rw + l32, n_rows - 1), qi = (int)a.by_group.quot(row);
   const int seen = keys_seen(a, t, qi);
   // keys up to which some, and all, rows of the wave see, and the workgroup's last one
-  const int seen_hi = rw < n_rows ? keys_seen(a, t, min(rw + 31, n_rows - 1) / a.group) : 0;
-  const int seen_lo = keys_seen(a, t, min(rw, n_rows - 1) / a.group);
-  const int kv_end = keys_seen(a, t, min(r0 + BQ - 1, n_rows - 1) / a.group);
+  const int seen_hi = rw < n_rows ? keys_seen(a, t, (int)a.by_group.quot(min(rw + 31, n_rows - 1))) : 0;
+  const int seen_lo = keys_seen(a, t, (int)a.by_group.quot(min(rw, n_rows - 1)));
+  const int kv_end = keys_seen(a, t, (int)a.by_group.quot(min(r0 + BQ - 1, n_rows - 1)));
 
-  // Q fragments: lane holds Q[row l32][kk*16 + hi*8 + 0..7]
-  bf16x8 qf[KK];
-  {
-    const bf16* qr = static_cast<const bf16*>(a.q) + (long)(t.q0 + qi) * a.q_stride +
-                     (long)(h * a.group + row - qi * a.group) * DH + hi * 8;
+  // Q fragments: lane holds Q[row l32][kk*16 + hi*8 + 0..7]. Half rows are loaded,
+  // a line at a time, and go through a part of the tile buffer that is loaded
+  // last (straight into this layout, 32 bytes of a row at a time, they took 1.2 us longer).
+  constexpr int QC = CPR / 2, QL = 32 * QC / 64;  // chunks of a half row, loads of the wave's half rows
+  bf16x8 qf[KK], qx[2][QL];
+  const int q_row = lane / QC, q_chunk = lane % QC;
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) qf[kk] = *reinterpret_cast<const bf16x8*>(qr + kk * 16);
-  }
+  for (int half = 0; half < 2; ++half)
+#pragma unroll
+    for (int i = 0; i < QL; ++i) {
+      const int R = min(rw + i * (64 / QC) + q_row, n_rows - 1), j = (int)a.by_group.quot(R);
+      qx[half][i] = *reinterpret_cast<const bf16x8*>(
+          static_cast<const bf16*>(a.q) + (long)(t.q0 + j) * a.q_stride +
+          (long)(h * a.group + R - j * a.group) * DH + (half * QC + q_chunk) * 8);
+    }
 
   // this lane's part of a tile load: segment seg = i*LW + wave, row seg*RPS + lane/CPR,
   // LDS slot lane%CPR holding global chunk slot ^ f(row). Loads come from waves
@@ -267,7 +274,7 @@ __global__ __launch_bounds__(NW * 64) void packed_large_kernel(PackedArgs a, Pac
   using B1 = std::integral_constant<int, 1>;
   using B2 = std::integral_constant<int, 2>;
   const int n_tiles = kv_end > 0 ? (kv_end + BKV - 1) / BKV : 0;
-  const int n_full = max(keys_seen(a, t, r0 / a.group), 0) / BKV;  // tiles that every row sees whole
+  const int n_full = max(keys_seen(a, t, (int)a.by_group.quot(r0)), 0) / BKV;  // tiles that every row sees whole
   // Where a row does not see a key its weight is 0, but 0 times an infinite
   // value is NaN. In the tiles that some row does not see whole, values that are not
   // finite are taken out by the wave that loaded them, and added to the rows that
@@ -290,6 +297,24 @@ __global__ __launch_bounds__(NW * 64) void packed_large_kernel(PackedArgs a, Pac
   if (n_tiles > 0) {
     issue_tile(B0{}, 0);
     if (n_tiles > 1) issue_tile(B1{}, BKV);
+    {
+      constexpr int EACH = 32 * QC * 8, PER = BKV * DH / EACH;  // values of a wave, waves to a buffer
+      static_assert(2 * PER >= NW, "two buffers hold the waves' half rows");
+      bf16* ql = (wave < PER ? K2 : V2) + wave % PER * EACH;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+#pragma unroll
+        for (int i = 0; i < QL; ++i) {
+          const int r = i * (64 / QC) + q_row;
+          *reinterpret_cast<bf16x8*>(ql + (r * QC + (q_chunk ^ (r & (QC - 1)))) * 8) = qx[half][i];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+#pragma unroll
+        for (int kk = 0; kk < KK / 2; ++kk)
+          qf[half * (KK / 2) + kk] = *reinterpret_cast<const bf16x8*>(ql + (l32 * QC + ((kk * 2 + hi) ^ (l32 & (QC - 1)))) * 8);
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+      }
+    }
     __builtin_amdgcn_s_waitcnt(waitcnt_vm(0));
     if (n_full == 0) take_odd(B0{});
     __syncthreads();
@@ -328,10 +353,12 @@ __global__ __launch_bounds__(NW * 64) void packed_large_kernel(PackedArgs a, Pac
 
   // acc[dt][e]: channel dt*32 + (e/4)*8 + hi*4 + e%4 of row l32
   const float l_tot = l_run + __shfl_xor(l_run, 32);
-  if (rw + l32 >= n_rows) return;
   const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
-  const int out_row = (t.q0 + qi) * (a.kv_heads * a.group) + h * a.group + (row - qi * a.group);  // below n_q * heads
-  bf16* dst = static_cast<bf16*>(a.o) + (long)out_row * DH;
+  // The rows go through LDS, so that whole lines of them are stored (8 bytes of
+  // a row at a time took 2 us longer).
+  __syncthreads();  // every wave is done with the tiles
+  constexpr int PER = BKV / 32;  // waves to a buffer
+  bf16* ol = (wave < PER ? K0 : (wave < 2 * PER ? K1 : K2)) + wave % PER * (32 * DH);
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
@@ -340,11 +367,22 @@ __global__ __launch_bounds__(NW * 64) void packed_large_kernel(PackedArgs a, Pac
       f32x4 v = {acc[dt][4 * g + 0] * inv, acc[dt][4 * g + 1] * inv, acc[dt][4 * g + 2] * inv,
                  acc[dt][4 * g + 3] * inv};
       if (cut_odd) add_odd(v, vg + c, a.v_stride, n_full * BKV, seen);
-      *reinterpret_cast<bf16x4*>(dst + c) = to_bf16x4(v);
+      *reinterpret_cast<bf16x4*>(ol + l32 * DH + (((dt * 4 + g) ^ (l32 & (CPR - 1))) * 8) + hi * 4) = to_bf16x4(v);
     }
   }
-  if (a.lse && hi == 0)
-    a.lse[out_row] = l_tot == 0.f ? -INFINITY : fmaf(m_ref, a.scale, __builtin_amdgcn_logf(l_tot) * kLn2);
+  __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+  auto head_row = [&](int R) -> long {  // of o and lse
+    const int i = (int)a.by_group.quot(R);
+    return (long)(t.q0 + i) * (a.kv_heads * a.group) + h * a.group + (R - i * a.group);
+  };
+#pragma unroll
+  for (int i = 0; i < 32 * CPR / 64; ++i) {
+    const int r = (i * 64 + lane) / CPR, c = lane % CPR;
+    const bf16x8 x = *reinterpret_cast<const bf16x8*>(ol + r * DH + ((c ^ (r & (CPR - 1))) * 8));
+    if (rw + r < n_rows) *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.o) + head_row(rw + r) * DH + c * 8) = x;
+  }
+  if (a.lse && hi == 0 && rw + l32 < n_rows)
+    a.lse[head_row(rw + l32)] = l_tot == 0.f ? -INFINITY : fmaf(m_ref, a.scale, __builtin_amdgcn_logf(l_tot) * kLn2);
 }
 
 template <int DH>

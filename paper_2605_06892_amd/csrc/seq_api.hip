@@ -178,6 +178,7 @@ HSA_API int hsa_packed_attention(int dtype, const void* q, int64_t q_stride, con
   a.n_kv = (int)n_kv;
   a.kv_heads = kv_heads;
   a.group = heads / kv_heads;
+  a.by_group = hsa::FastDiv((uint32_t)a.group);
   a.scale = scale;
   a.causal = causal != 0;
   a.o = o;

@@ -48,6 +48,7 @@ struct PackedArgs {
   const int32_t *cu_q, *cu_kv;
   int n_seqs, n_q, n_kv;
   int kv_heads, group;  // heads = kv_heads * group
+  FastDiv by_group;
   float scale;
   int causal;
   void* o;
