@@ -591,8 +591,8 @@ int hsa_cache_store(int dtype, const void* k, int64_t k_stride, const void* v, i
  * j < n, in dtype (exact: the codes' values for HSA_STEP_E4M3, a copy
  * otherwise). An index may come twice; one outside [0, n_rows) gives a row of
  * zeros. Arguments as for hsa_cache_store; k and v must not overlap the caches,
- * the exponents, idx or each other (rows between the strides are left as they
- * were, and k and v may interleave only if their spans do not overlap).
+ * the exponents, idx or each other, each taken from its first row to the end
+ * of its last (what lies between the rows is left as it was).
  */
 int hsa_cache_load(int cache_dtype, const void* k_cache, const void* v_cache, const int8_t* k_exp,
                    const int8_t* v_exp, const int32_t* idx, int32_t n, int64_t n_rows,
@@ -619,7 +619,7 @@ int hsa_cache_load(int cache_dtype, const void* k_cache, const void* v_cache, co
  *   o           [n_q, heads * head_dim] dtype, contiguous
  *   lse         NULL or [n_q, heads] fp32
  *   scale       > 0, finite
- * n_q * heads / 16 + (n_seqs + 8) * kv_heads < 2^23. o and lse must not overlap an input or
+ * n_q * heads / 16 + (n_seqs + 8) * kv_heads < 2^23, n_kv <= 2^30. o and lse must not overlap an input or
  * each other.
  */
 int hsa_packed_attention(int dtype, const void* q, int64_t q_stride, const void* k,
@@ -658,7 +658,7 @@ size_t hsa_paged_attention_workspace_bytes(int dtype, int32_t n_seqs, int32_t he
  *                n_seqs, heads, kv_heads, head_dim, max_pages * page_size)
  *                bytes, 16-byte aligned, overwritten; NULL where that is 0. Calls
  *                that may overlap in time need one each; nothing in it has to start at zero.
- * page_size >= 1; n_pages * page_size and max_pages * page_size < 2^31, n_seqs * heads < 2^23.
+ * page_size >= 1; n_pages * page_size < 2^31, max_pages * page_size <= 2^30, n_seqs * heads < 2^23.
  * o and lse must not overlap an input, the workspace or each other.
  */
 int hsa_paged_attention(int dtype, const void* q, int64_t q_stride, int cache_dtype,

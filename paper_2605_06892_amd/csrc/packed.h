@@ -52,53 +52,64 @@ __device__ __forceinline__ void packed_place(const PackedGrid& g, int& head, int
   tile = xcd / c + g.share * (g.turns ? x : y);
 }
 
-// Tile `idx` of the batch: the sequences one after the other, and within a
-// sequence the last tile first (under a causal mask the longest). Up to 64 sequences
-// come in the order of their tiles, the longest first, so that what runs last is
-// short; more come as they are. False past the last tile. Whatever the offsets hold, the rows are
-// inside [0, n_q) and [0, n_kv). Called by whole waves; the result is the same in every lane.
-__device__ __forceinline__ bool find_tile(const PackedArgs& a, int idx, int rows, SeqTile& t) {
+// Rows of sequence `s`, inside [0, n) whatever the offsets hold.
+__device__ __forceinline__ void seq_rows(const int32_t* cu, int s, int n, int& from, int& to) {
+  from = min(max(cu[s], 0), n);
+  to = min(max(cu[s + 1], from), n);
+}
+
+// Tile `idx` of the batch; false for one that no sequence has. Within a sequence
+// the last tile comes first (under a causal mask the longest). Called by whole
+// waves; the result is the same in every lane.
+//   Up to 64 sequences, one to a lane: in the order of their tiles, the longest
+//   first, so that what runs last is short.
+//   More: as they are, sequence s from tile floor(cu_q[s] G / ROWS) + s on, which leaves
+//   each at least its tiles; found by probing 64 sequences at a time.
+template <int ROWS>
+__device__ __forceinline__ bool find_tile(const PackedArgs& a, int idx, SeqTile& t) {
   const int lane = threadIdx.x & (kWave - 1);
-  for (int s0 = 0; s0 < a.n_seqs; s0 += kWave) {
-    const int s = s0 + lane;
+  if (a.n_seqs <= kWave) {
     int q0 = 0, q1 = 0, k0 = 0, k1 = 0;
-    if (s < a.n_seqs) {
-      q0 = min(max(a.cu_q[s], 0), a.n_q);
-      q1 = min(max(a.cu_q[s + 1], q0), a.n_q);
-      k0 = min(max(a.cu_kv[s], 0), a.n_kv);
-      k1 = min(max(a.cu_kv[s + 1], k0), a.n_kv);
+    if (lane < a.n_seqs) {
+      seq_rows(a.cu_q, lane, a.n_q, q0, q1);
+      seq_rows(a.cu_kv, lane, a.n_kv, k0, k1);
     }
-    const int tiles = (int)(((long)(q1 - q0) * a.group + rows - 1) / rows);
-    int from = 0, all = 0;  // tiles before this lane's sequence, and of the 64
-    if (a.n_seqs <= kWave) {
-      for (int i = 0; i < a.n_seqs; ++i) {
-        const int n = __builtin_amdgcn_readlane(tiles, i);
-        from += n > tiles || (n == tiles && i < lane) ? n : 0;
-        all += n;
-      }
-    } else {
-      all = tiles;
-#pragma unroll
-      for (int o = 1; o < kWave; o <<= 1) {
-        const int y = __shfl_up(all, o);
-        if (lane >= o) all += y;
-      }
-      from = all - tiles;
-      all = __builtin_amdgcn_readlane(all, kWave - 1);
+    const int tiles = (int)(((long)(q1 - q0) * a.group + ROWS - 1) / ROWS);
+    int from = 0;  // tiles before this lane's sequence
+    for (int i = 0; i < a.n_seqs; ++i) {
+      const int n = __builtin_amdgcn_readlane(tiles, i);
+      from += n > tiles || (n == tiles && i < lane) ? n : 0;
     }
     const unsigned long hit = __ballot(from <= idx && idx < from + tiles);
-    if (hit) {
-      const int l = __builtin_ctzl(hit);
-      t.q0 = __builtin_amdgcn_readlane(q0, l);
-      t.len_q = __builtin_amdgcn_readlane(q1, l) - t.q0;
-      t.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - (idx - __builtin_amdgcn_readlane(from, l));
-      t.k0 = __builtin_amdgcn_readlane(k0, l);
-      t.len_k = __builtin_amdgcn_readlane(k1, l) - t.k0;
-      return true;
-    }
-    idx -= all;
+    if (!hit) return false;
+    const int l = __builtin_ctzl(hit);
+    t.q0 = __builtin_amdgcn_readlane(q0, l);
+    t.len_q = __builtin_amdgcn_readlane(q1, l) - t.q0;
+    t.k0 = __builtin_amdgcn_readlane(k0, l);
+    t.len_k = __builtin_amdgcn_readlane(k1, l) - t.k0;
+    t.tile = __builtin_amdgcn_readlane(tiles, l) - 1 - (idx - __builtin_amdgcn_readlane(from, l));
+    return true;
   }
-  return false;
+  auto first = [&](int s) { return (int)((long)min(max(a.cu_q[s], 0), a.n_q) * a.group / ROWS) + s; };
+  int lo = 0;  // the last sequence whose first tile is at most idx is one of lo .. lo+n-1
+  for (int n = a.n_seqs; n > 1;) {
+    const int step = (n + kWave - 1) / kWave;
+    const unsigned long below = __ballot(lane * step < n && first(lo + min(lane * step, n - 1)) <= idx);
+    if (!below) return false;
+    const int l = kWave - 1 - __builtin_clzl(below);
+    lo += l * step;
+    n = min(step, n - l * step);
+  }
+  int q1, k1;
+  seq_rows(a.cu_q, lo, a.n_q, t.q0, q1);
+  seq_rows(a.cu_kv, lo, a.n_kv, t.k0, k1);
+  t.q0 = __builtin_amdgcn_readfirstlane(t.q0);
+  t.len_q = __builtin_amdgcn_readfirstlane(q1) - t.q0;
+  t.k0 = __builtin_amdgcn_readfirstlane(t.k0);
+  t.len_k = __builtin_amdgcn_readfirstlane(k1) - t.k0;
+  const int tiles = (int)(((long)t.len_q * a.group + ROWS - 1) / ROWS);
+  t.tile = tiles - 1 - (idx - __builtin_amdgcn_readfirstlane(first(lo)));
+  return t.tile >= 0 && t.tile < tiles;
 }
 
 // keys that query i of the sequence sees (at most 0: none)

@@ -66,7 +66,7 @@ __global__ __launch_bounds__(NW * 64) void packed_small_kernel(PackedArgs a, Pac
   int h, idx;
   SeqTile t;
   packed_place(grid, h, idx);
-  if (!find_tile(a, idx, W, t)) return;
+  if (!find_tile<W>(a, idx, t)) return;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lw = lane % W, slot = lane / W;
@@ -264,21 +264,21 @@ hipError_t launch_small(const PackedArgs& a, hipStream_t s) {
 }
 
 // Fitted to 499 launches of 1, 5 and 20 prompts of 1 to 4500 tokens, with and without 1000
-// rows before them, 1 to 40 heads of either width: the least estimate takes 1.5% more
-// than the fastest of the five on average, over 10% more in one launch of 20. Measured, 128-wide
-// heads, in this order: 8 heads, 1 prompt of 400 tokens 9.7, 10.3, 11.1, 12.0 and 16.7;
-// of 1000 20.5, 19.2, 17.7, 19.5 and 30.0; of 4500 224, 217, 137, 139 and 100;
-// 20 prompts of 25 to 77, 8 heads 14.9, 12.1, 13.2, 14.8 and 9.3.
-constexpr PackedCost kCosts[2][5] = {{{16, 8, 2.6, 2.3, 0.127, 0.141},   // 64-wide heads
-                                      {16, 4, 3.9, 0.93, 0.142, 0.05},
-                                      {32, 8, 0.0, 5.3, 0.164, 0.026},
-                                      {32, 4, 2.8, 2.6, 0.161, 0.203},
-                                      {256, 8, 0.0, 6.7, 0.513, 0.332}},
-                                     {{16, 8, 0.0, 5.4, 0.289, 0.08},    // 128-wide
-                                      {16, 4, 3.3, 2.4, 0.272, 0.125},
-                                      {32, 8, 0.0, 6.4, 0.346, 0.161},
-                                      {32, 4, 0.0, 6.9, 0.348, 0.298},
-                                      {256, 8, 0.0, 8.0, 0.78, 0.487}}};
+// rows before them, 1 to 40 heads of either width: the least estimate takes 1.2% more
+// than the fastest of the five on average, over 10% more in one launch of 38. Measured, 128-wide
+// heads, in this order: 8 heads, no mask, 1 prompt of 400 tokens 10.2, 10.2, 11.8, 12.2 and 15.8;
+// of 1000 29.2, 26.8, 19.0, 18.6 and 28.6; of 4500 395, 366, 241, 247 and 103; causal, 20 prompts
+// of 25 to 77 15.1, 10.6, 12.1, 13.1 and 10.0.
+constexpr PackedCost kCosts[2][5] = {{{16, 8, 2.6, 2.2, 0.130, 0.144},   // 64-wide heads
+                                      {16, 4, 3.9, 0.85, 0.145, 0.05},
+                                      {32, 8, 0.0, 5.1, 0.169, 0.021},
+                                      {32, 4, 2.7, 2.5, 0.161, 0.202},
+                                      {256, 8, 0.0, 6.9, 0.490, 0.244}},
+                                     {{16, 8, 0.0, 5.2, 0.291, 0.05},    // 128-wide
+                                      {16, 4, 3.2, 2.4, 0.272, 0.116},
+                                      {32, 8, 0.0, 6.2, 0.353, 0.175},
+                                      {32, 4, 0.0, 6.6, 0.340, 0.292},
+                                      {256, 8, 0.0, 8.2, 0.713, 0.05}}};
 
 template <int DH>
 hipError_t launch_dh(const PackedArgs& a, hipStream_t s) {

@@ -50,7 +50,7 @@ __global__ __launch_bounds__(NW * kWave, DH == 64 ? 4 : 2) void packed_f32_kerne
   int h, idx;
   SeqTile t;
   packed_place(grid, h, idx);
-  if (!find_tile(a, idx, W, t)) return;
+  if (!find_tile<W>(a, idx, t)) return;
 
   const int lane = threadIdx.x & (kWave - 1);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);

@@ -73,7 +73,7 @@ __global__ __launch_bounds__(NW * 64) void packed_large_kernel(PackedArgs a, Pac
   int h, idx;
   SeqTile t;
   packed_place(grid, h, idx);
-  if (!find_tile(a, idx, BQ, t)) return;
+  if (!find_tile<BQ>(a, idx, t)) return;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);  // uniform: scalar
   const int l32 = lane & 31, hi = lane >> 5;

@@ -9,8 +9,8 @@
 // loads the CUs evenly and one long sequence is spread over all of them. A run that holds a
 // whole item writes its output; the first and the last item of a run may be parts, which
 // go to the workspace (unnormalized output, maximum and sum of the softmax) and are
-// joined by a second kernel. Where each item begins follows from the lengths alone, and both
-// kernels work it out for themselves: no atomics, no state between calls.
+// joined by a second kernel. Every run works out from the lengths where it begins, and leaves
+// a note of the item that it begins and does not end: no atomics, no state between calls.
 //
 // In a workgroup, each wave takes every NW-th block of the item's rows, 32 keys
 // of bf16 or e4m3 rows (16 with fp32 queries), one block loaded ahead (its page one more
@@ -113,6 +113,16 @@ struct Part {  // a part of an item in the workspace
   float o[kRows * DH];
   float ml[kRows * 2];
 };
+// The item that a run begins and does not end: its parts are this run's in
+// `slot` and the next `more` runs' first (0: there is no such item). In the workspace
+// behind the parts, two to a run.
+struct Note {
+  int s, item, slot, more;
+};
+template <int DH>
+__device__ __forceinline__ Note* notes(const PagedArgs& a, const Plan& plan) {
+  return reinterpret_cast<Note*>(static_cast<Part<DH>*>(a.ws) + 2 * (long)plan.wgs);
+}
 
 // exp((x - y) * scale) for x <= y, as exact as the form needs
 template <bool F32>
@@ -474,6 +484,7 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void paged_split_kernel(PagedA
   walk.view(a, per, 0, 0);
   const long total = all_tiles(a, per, walk), run = run_tiles(total, plan.wgs);
   const long begin = run * blockIdx.x, end = min(total, begin + run);
+  Note note{0, 0, 0, 0};
   for (long pos = begin; pos < end;) {
     const int l = walk.find(a, per, pos);
     if (l < 0) break;  // lengths that changed under the call
@@ -483,47 +494,35 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void paged_split_kernel(PagedA
     const int t0 = uniform((int)(off - (long)item * tiles));
     const int n_t = uniform((int)min((long)(tiles - t0), end - pos));
     const int h = item / plan.gts;
-    Part<DH>* part = n_t == tiles ? nullptr : static_cast<Part<DH>*>(a.ws) + 2 * (long)blockIdx.x + (pos == begin ? 0 : 1);
+    const int slot = pos == begin ? 0 : 1;
+    Part<DH>* part = n_t == tiles ? nullptr : static_cast<Part<DH>*>(a.ws) + 2 * (long)blockIdx.x + slot;
+    if (t0 == 0 && n_t < tiles)  // the run ends here
+      note = Note{s, item, slot, (int)min(div_pos(pos + tiles - 1, run), (long)plan.wgs - 1) - (int)blockIdx.x};
     A::run(a, plan, sh, s, h, (item - h * plan.gts) * kRows, t0 * kTile, min(len, (t0 + n_t) * kTile), part);
     pos += n_t;
     if (pos < end) __syncthreads();  // the merge has read what the next item writes
   }
+  if (threadIdx.x == 0) notes<DH>(a, plan)[blockIdx.x] = note;
 }
 
-// The output of items that more than one run holds, one query head per workgroup:
-// its threads take 4 channels each of every few parts, then join those.
+// The output of the item that run blockIdx.x begins and does not end, one query
+// head per workgroup: its threads take 4 channels each of every few parts, then join those.
 template <bool F32, int DH>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a, Plan plan) {
   constexpr int C = DH / 4, G = kJoinThreads / C;  // threads per part, parts at a time
   __shared__ __attribute__((aligned(16))) f32x4 sums[G][C];
   __shared__ float ms[G], ls[G];
-  const int heads = a.kv_heads * a.group, per = a.kv_heads * plan.gts;
-  const int s = blockIdx.x / heads, hq = blockIdx.x - s * heads;
-  const int h = hq / a.group, g = hq - h * a.group, item = h * plan.gts + g / kRows, r = g % kRows;
-  Walk walk;
-  walk.view(a, per, 0, 0);
-  const long total = all_tiles(a, per, walk), run = run_tiles(total, plan.wgs);
-  long before = 0;  // tiles before the sequence
-  if (a.n_seqs <= kWave) {
-    before = __shfl(walk.from, s);
-  } else {
-    for (int i = threadIdx.x & (kWave - 1); i < s; i += kWave) before += tiles_of(seq_len(a, i));
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) before += __shfl_xor(before, o);
-    before *= per;
-  }
-  const int tiles = tiles_of(seq_len(a, s));
-  const long first = before + (long)item * tiles;
-  const int w0 = (int)div_pos(first, run), w1 = (int)div_pos(first + tiles - 1, run);
-  if (w0 == w1) return;
+  const int w0 = blockIdx.x, r = blockIdx.y;
+  const Note note = notes<DH>(a, plan)[w0];
+  const int h = note.item / plan.gts, g = (note.item - h * plan.gts) * kRows + r;
+  if (note.more == 0 || g >= a.group) return;
   const Part<DH>* parts = static_cast<const Part<DH>*>(a.ws);
   const int lane_p = threadIdx.x / C, c = (threadIdx.x - lane_p * C) * 4;
   float m = -INFINITY, l = 0.f;
   f32x4 sum = {};
 #pragma unroll 4
-  for (int w = w0 + lane_p; w <= w1; w += G) {
-    // the item is the last of its first run and the first of every other
-    const Part<DH>* p = parts + 2 * (long)w + (w > w0 || run * w == first ? 0 : 1);
+  for (int i = lane_p; i <= note.more; i += G) {
+    const Part<DH>* p = parts + 2 * (long)(w0 + i) + (i ? 0 : note.slot);
     const f32x2 ml = *reinterpret_cast<const f32x2*>(&p->ml[2 * r]);
     const f32x4 x = *reinterpret_cast<const f32x4*>(&p->o[r * DH + c]);
     if (ml[0] == -INFINITY && ml[1] == 0.f) continue;  // no key, or no finite score
@@ -552,7 +551,7 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a, P
     l = fmaf(wt, ls[i], l);
     sum += wt * sums[i][c / 4];
   }
-  write_out<F32, DH>(a, (long)s * heads + hq, c, m_all, l, sum);
+  write_out<F32, DH>(a, (long)note.s * (a.kv_heads * a.group) + h * a.group + g, c, m_all, l, sum);
 }
 
 int gts_of(int group) { return (group + kRows - 1) / kRows; }
@@ -581,8 +580,7 @@ hipError_t launch(const PagedArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((paged_split_kernel<F32, E4M3, DH, ALIGNED>), dim3(plan.wgs), dim3(kSplitWaves * 64), 0, s, a, plan);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((paged_join_kernel<F32, DH>), dim3((unsigned)(a.n_seqs * a.kv_heads * a.group)), dim3(kJoinThreads), 0,
-                     s, a, plan);
+  hipLaunchKernelGGL((paged_join_kernel<F32, DH>), dim3(plan.wgs, std::min(a.group, kRows)), dim3(kJoinThreads), 0, s, a, plan);
   return hipGetLastError();
 }
 
@@ -597,7 +595,7 @@ hipError_t launch_held(const PagedArgs& a, bool e4m3, hipStream_t s) {
 
 size_t paged_attention_bytes(int n_seqs, int kv_heads, int group, int head_dim, long max_len) {
   if (n_seqs <= 0 || !splits(max_len)) return 0;
-  return (size_t)workgroups(n_seqs, kv_heads, group, max_len) * 2 * kRows * (head_dim + 2) * sizeof(float);
+  return (size_t)workgroups(n_seqs, kv_heads, group, max_len) * (2 * kRows * (head_dim + 2) * sizeof(float) + sizeof(Note));
 }
 
 hipError_t launch_paged_attention(const PagedArgs& a, bool bf16, bool e4m3, int head_dim, hipStream_t s) {

@@ -10,6 +10,7 @@ using namespace hsa_api;
 namespace {
 
 constexpr int64_t kMaxStride = int64_t(1) << 22;  // elements between rows
+constexpr int64_t kMaxKeys = int64_t(1) << 30;    // keys of a sequence, so that a position plus a block fits an int
 constexpr int64_t kMaxLaunch = int64_t(1) << 32;  // threads of one launch
 
 // Bytes from the first to the end of the last of n rows `stride` elements apart.
@@ -150,7 +151,7 @@ HSA_API int hsa_packed_attention(int dtype, const void* q, int64_t q_stride, con
   const size_t es = elem_size(dtype);
   if (!es) return HSA_STEP_ERR_DTYPE;
   if (!heads_ok(heads, kv_heads, head_dim) || n_seqs < 0 || n_seqs == INT32_MAX || n_q < 0 || n_kv < 0 ||
-      n_q > kMaxRows / heads || n_kv > kMaxRows || !(scale > 0.f) || !isfinite(scale))
+      n_q > kMaxRows / heads || n_kv > kMaxKeys || !(scale > 0.f) || !isfinite(scale))
     return HSA_STEP_ERR_SHAPE;
   // one launch: fewer than 2^32 threads, 512 per 16 rows or item
   if (n_q * heads / 16 + ((int64_t)n_seqs + 8) * kv_heads >= kMaxLaunch / 512) return HSA_STEP_ERR_SHAPE;
@@ -190,7 +191,7 @@ HSA_API size_t hsa_paged_attention_workspace_bytes(int dtype, int32_t n_seqs, in
                                                    int32_t kv_heads, int32_t head_dim,
                                                    int64_t max_len) {
   if (!elem_size(dtype) || !heads_ok(heads, kv_heads, head_dim) || n_seqs < 0 || max_len < 0 ||
-      max_len > kMaxRows || n_seqs > kMaxRows / heads)
+      max_len > kMaxKeys || n_seqs > kMaxRows / heads)
     return 0;
   return hsa::paged_attention_bytes(n_seqs, kv_heads, heads / kv_heads, head_dim, max_len);
 }
@@ -206,7 +207,7 @@ HSA_API int hsa_paged_attention(int dtype, const void* q, int64_t q_stride, int 
   if (!es || !ce) return HSA_STEP_ERR_DTYPE;
   if (!heads_ok(heads, kv_heads, head_dim) || n_seqs < 0 || n_seqs > kMaxRows / heads || n_pages < 0 ||
       max_pages < 0 || page_size < 1 || (int64_t)n_pages * page_size > kMaxRows ||
-      (int64_t)max_pages * page_size > kMaxRows || !(scale > 0.f) || !isfinite(scale))
+      (int64_t)max_pages * page_size > kMaxKeys || !(scale > 0.f) || !isfinite(scale))
     return HSA_STEP_ERR_SHAPE;
   const int64_t d = (int64_t)heads * head_dim, dk = (int64_t)kv_heads * head_dim;
   const int64_t n_rows = (int64_t)n_pages * page_size;

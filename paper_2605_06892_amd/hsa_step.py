@@ -441,6 +441,15 @@ def _here() -> int:
         return -2
 
 
+def _stream_here(stream, dev: int):
+    """The stream's handle: the current one of device dev, or a given one of that device."""
+    if stream is None:
+        return _raw_stream(dev) if _raw_stream else torch.cuda.current_stream().cuda_stream
+    if stream.device_index != dev:
+        raise ValueError(f"the stream must be of the current device (cuda:{dev}), got {stream.device}")
+    return stream.cuda_stream
+
+
 def _held(dev: int, *ts) -> bool:
     """Contiguous tensors on the device."""
     for t in ts:
@@ -504,7 +513,7 @@ def _cache_call(name: str, k, v, idx, n: int, kv_heads: int, kc, vc, ke, ve, str
     dt = _DTYPES[dt]
     rows = (k.data_ptr(), kst[0] if ksh[0] > 1 else ksh[1], v.data_ptr(), vst[0] if vsh[0] > 1 else vsh[1])
     kep, vep = (ke.data_ptr(), ve.data_ptr()) if e4m3 else (None, None)
-    stream = _stream(stream)
+    stream = _stream_here(stream, dev)
     if name == "hsa_cache_store":
         st = lib().hsa_cache_store(dt, *rows, idx.data_ptr(), n, csh[0], kv_heads, csh[1] // kv_heads,
                                    E4M3 if e4m3 else dt, kc.data_ptr(), vc.data_ptr(), kep, vep, stream)
@@ -552,7 +561,7 @@ def hsa_packed_attention(q, k, v, cu_q, cu_kv, heads: int, kv_heads: int, head_d
                                     kst[0] if n_kv > 1 else ksh[1], v.data_ptr(), vst[0] if n_kv > 1 else ksh[1],
                                     cu_q.data_ptr(), cu_kv.data_ptr(), n_seqs, n_q, n_kv, heads, kv_heads, head_dim, scale,
                                     1 if causal else 0, o.data_ptr(), None if lse is None else lse.data_ptr(),
-                                    _stream(stream))
+                                    _stream_here(stream, dev))
     if st:
         raise HsaStepError("hsa_packed_attention", st)
 
@@ -596,7 +605,7 @@ def hsa_paged_attention(q, k_cache, v_cache, page_table, kv_lens, page_size: int
                                    None if lse is None else lse.data_ptr(),
                                    None if workspace is None else workspace.data_ptr(),
                                    0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                   _stream(stream))
+                                   _stream_here(stream, dev))
     if st:
         raise HsaStepError("hsa_paged_attention", st)
 

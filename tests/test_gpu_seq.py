@@ -18,6 +18,7 @@ import torch
 
 from gpu_util import Guarded
 from paper_2605_06892_amd import hsa_step as H
+from paper_2605_06892_amd import paged
 
 pytestmark = pytest.mark.gpu
 
@@ -164,6 +165,64 @@ def test_packed_many_sequences(form):
     o, lse = run_packed(q, k, v, cu_q, cu_k, 4, 2, 64, 0.125, True)
     want, lw, A, S = packed_want(q, k, v, cu_q, cu_k, 4, 2, 64, 0.125, True)
     check(o, lse, want, lw, A, S, dtype, 23, 64)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_packed_thousands_of_sequences(form, causal):
+    """More than 64 x 64 of them, of no to 3 tokens, behind rows of no sequence."""
+    dtype = form
+    lens = [(i * 7) % 4 for i in range(4500)]
+    q, k, v, cu_q, cu_k = packed_inputs(4, dtype, lens, lens, 2, 1, 64, 37, 5)
+    o, lse = (torch.full((q.shape[0], w), 7.0, dtype=t, device=DEV) for w, t in ((128, T[dtype]), (2, torch.float32)))
+    run_packed(q, k, v, cu_q, cu_k, 2, 1, 64, 0.125, causal, o, lse)
+    want, lw, A, S = packed_want(q, k, v, cu_q, cu_k, 2, 1, 64, 0.125, causal)
+    rows = slice(37, 37 + sum(lens))
+    check(o[rows], lse[rows], want[rows], lw[rows], A[rows], S, dtype, 3, 64)
+    assert torch.all(o[:37] == 7.0) and torch.all(o[rows.stop:] == 7.0)
+
+
+def test_packed_without_keys(form):
+    dtype = form
+    q = torch.ones(5, 128, dtype=T[dtype], device=DEV)
+    k = torch.empty(0, 128, dtype=T[dtype], device=DEV)
+    cu = torch.tensor([0, 2, 5], dtype=torch.int32, device=DEV)
+    o, lse = torch.full_like(q, 7.0), torch.full((5, 1), 7.0, device=DEV)
+    H.hsa_packed_attention(q, k, k, cu, torch.zeros_like(cu), 1, 1, 128, 0.1, False, o, lse=lse)
+    assert torch.all(o == 0) and torch.all(lse == -math.inf)
+    H.hsa_packed_attention(q[:0], k, k, cu, cu, 1, 1, 128, 0.1, False, o[:0])           # no queries
+    H.hsa_packed_attention(q, k, k, cu[:1], cu[:1], 1, 1, 128, 0.1, False, o.fill_(7.0))  # no sequences
+    assert torch.all(o == 7.0)
+
+
+def off_by_one(t):
+    """The tensor at an address that is a multiple of 4 bytes and no more."""
+    raw = torch.empty(t.numel() + 1, dtype=t.dtype, device=DEV)
+    x = raw[1:].view(t.shape)
+    x.copy_(t)
+    return x
+
+
+def test_f32_rows_of_4_byte_alignment():
+    """fp32 tensors off the 16-byte alignment, through every call."""
+    heads, kv, dh, n, page = 4, 2, 64, 150, 8
+    g = _gen(21)
+    q, k, v = (off_by_one(_randn(g, n, w * dh)) for w in (heads, kv, kv))
+    cu = torch.tensor([0, 47, n], dtype=torch.int32)
+    o, lse = off_by_one(torch.zeros(n, heads * dh)), torch.empty(n, heads, device=DEV)
+    cud = cu.to(DEV)
+    H.hsa_packed_attention(q, k, v, cud, cud, heads, kv, dh, 0.125, True, o, lse=lse)
+    want, lw, A, S = packed_want(q.cpu(), k.cpu(), v.cpu(), cu, cu, heads, kv, dh, 0.125, True)
+    check(o, lse, want, lw, A, S, "f32", n, dh)
+    kc, vc = (off_by_one(torch.zeros(160, kv * dh)) for _ in range(2))
+    idx = torch.randperm(160, generator=g)[:n].to(torch.int32)
+    H.hsa_cache_store(k, v, idx.to(DEV), n, kv, kc, vc)
+    k2, v2 = (off_by_one(torch.zeros(n, kv * dh)) for _ in range(2))
+    H.hsa_cache_load(kc, vc, idx.to(DEV), n, kv, k2, v2)
+    assert torch.equal(k, k2) and torch.equal(v, v2)
+    table = torch.randperm(20, generator=g).view(1, 20).to(torch.int32)
+    o1, l1 = run_paged(off_by_one(q[:1].cpu()), (kc, vc, None, None), table, [155], page, heads, kv, dh, 0.125)
+    want, lw, A, S = paged_want(q[:1].cpu(), kc.cpu(), vc.cpu(), table, [155], page, 20, heads, kv, dh, 0.125)
+    check(o1, l1, want, lw, A, S, "f32", 155, dh)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -587,6 +646,34 @@ def test_paged_shared_pages_odd_rows_and_long_lengths(dtype, cache, page):
         check(o, lse, want, lw, A, S, dtype, full, dh)
 
 
+@pytest.mark.parametrize("max_pages", [0, 3, 300])
+def test_paged_without_rows(max_pages):
+    """No pages in the table, and no pages in the cache: outputs of zeros."""
+    q = torch.ones(2, 256, dtype=torch.bfloat16, device=DEV)
+    c = torch.empty(0, 128, dtype=torch.bfloat16, device=DEV)
+    table = torch.zeros(2, max_pages, dtype=torch.int32)
+    o, lse = run_paged(q, (c, c, None, None), table, [5, 0], 16, 2, 1, 128, 0.1)
+    assert torch.all(o == 0) and torch.all(lse == -math.inf)
+
+
+@pytest.mark.parametrize("cache", ["bf16", "e4m3"])
+def test_paged_length_at_the_limit(cache):
+    """The longest length the call takes, 2^22 pages of 256 rows, all of them the same page but for the first. Its
+    2048 waves add up 2^17 weights in each lane, so sums are off by 2^17 u of themselves at most."""
+    q, k, v, held, table = paged_inputs(31, "bf16", cache, [512], 256, 2, 1, 64, spare=0)
+    n = 2 ** 30
+    table = torch.full((1, n // 256), int(table[0, 1]), dtype=torch.int32).index_fill(1, torch.tensor([0]), int(table[0, 0]))
+    o, lse = run_paged(q, held, table, [n], 256, 2, 1, 64, 0.125)
+    first, rest = int(table[0, 0]) * 256, int(table[0, 1]) * 256
+    for h in range(2):
+        # every row of the second page counts 2^22 - 1 times
+        s = [(k[r:r + 256].double() @ q[0, h * 64:h * 64 + 64].double()) * 0.125 for r in (first, rest)]
+        w = torch.cat([s[0], s[1] + math.log(n // 256 - 1)])
+        want = torch.softmax(w, 0) @ torch.cat([v[first:first + 256], v[rest:rest + 256]]).double()
+        assert float((o[0, h * 64:h * 64 + 64].cpu().double() - want).abs().max()) < (2.0 ** -7 + 2 ** 18 * U) * float(v.abs().max())
+        assert abs(float(lse[0, h]) - float(torch.logsumexp(w, 0))) < 2 ** 17 * U + 1e-5
+
+
 def test_paged_odd_values_that_are_seen():
     lens, page = [200, 40], 16
     q, k, v, held, table = paged_inputs(7, "bf16", "bf16", lens, page, 2, 1, 64)
@@ -683,6 +770,41 @@ def test_prompts_then_tokens(dtype, cache):
             held.append(rows)
         want, lw, A, S = paged_want(q1, held[0], held[1], table, lens, page, n * width, heads, kv, dh, scale)
         check(o, lse, want, lw, A, S, dtype, max(lens), dh)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_paged_cache_module(e4m3):
+    """paged.prefill and paged.decode against one causal pass over the whole sequences: the last rows of a prompt
+    that is one longer are what the decoding step gives."""
+    heads, kv, dh, page = 8, 2, 128, 32
+    prompts = [40, 3, 97]
+    g = _gen(14)
+    c = paged.PagedCache.allocate(20, page, kv, dh, torch.bfloat16, e4m3=e4m3)
+    pages = torch.randperm(20, generator=g).numpy()[:12].reshape(3, 4).astype(np.int32)
+    full = [[_randn(g, p + 1, w * dh).bfloat16() for w in (heads, kv, kv)] for p in prompts]
+    if e4m3:  # keys and values that 8 bits hold, so that both passes see the same
+        for f in full:
+            for j in (1, 2):
+                codes, ex = quantize64(f[j], kv)
+                f[j] = (codes.view(-1, kv, dh) * torch.pow(2.0, ex.double())[..., None]).view(f[j].shape).bfloat16()
+    q, k, v = (torch.cat([f[i][:p] for f, p in zip(full, prompts)]).to(DEV) for i in range(3))
+    cu = torch.tensor(np.cumsum([0] + prompts), dtype=torch.int32, device=DEV)
+    idx = paged.slots(pages, page, np.repeat(np.arange(3), prompts), np.concatenate([np.arange(p) for p in prompts]))
+    o = torch.empty_like(q)
+    paged.prefill(c, q, k, v, cu, torch.from_numpy(idx).to(DEV), heads, o)
+    q1, k1, v1 = (torch.stack([f[i][-1] for f in full]).to(DEV) for i in range(3))
+    idx = paged.slots(pages, page, np.arange(3), np.array(prompts))
+    o1 = torch.empty_like(q1)
+    lens = torch.tensor([p + 1 for p in prompts], dtype=torch.int32, device=DEV)
+    paged.decode(c, q1, k1, v1, torch.from_numpy(idx).to(DEV), torch.from_numpy(pages).to(DEV), lens, heads, o1)
+    qa, ka, va = (torch.cat([f[i] for f in full]) for i in range(3))
+    cu = torch.tensor(np.cumsum([0] + [p + 1 for p in prompts]), dtype=torch.int32)
+    want, lw, A, S = packed_want(qa, ka, va, cu, cu, heads, kv, dh, c.scale, True)
+    last = cu[1:].long() - 1
+    rest = torch.ones(len(qa), dtype=torch.bool)
+    rest[last] = False
+    check(o, None, want[rest], None, A[rest], S, "bf16", 98, dh)
+    check(o1, None, want[last], None, A[last], S, "bf16", 98, dh)
 
 
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])

@@ -75,7 +75,7 @@ PACKED = dict(dtype=BF16, q=P[0], q_stride=2048, k=P[1], k_stride=512, v=P[2], v
     (dict(kv_heads=3), SHAPE), (dict(heads=0), SHAPE), (dict(kv_heads=0), SHAPE), (dict(kv_heads=-4), SHAPE),
     (dict(heads=-16, kv_heads=-4), SHAPE), (dict(head_dim=32), SHAPE), (dict(head_dim=256), SHAPE),
     (dict(n_seqs=-1), SHAPE), (dict(n_seqs=2 ** 31 - 1), SHAPE), (dict(n_q=-1), SHAPE), (dict(n_kv=-1), SHAPE),
-    (dict(n_q=2 ** 31 - 1), SHAPE), (dict(n_q=2 ** 62), SHAPE), (dict(n_kv=2 ** 31), SHAPE),
+    (dict(n_q=2 ** 31 - 1), SHAPE), (dict(n_q=2 ** 62), SHAPE), (dict(n_kv=2 ** 31), SHAPE), (dict(n_kv=2 ** 30 + 1), SHAPE),
     (dict(n_q=2 ** 24), SHAPE), (dict(n_seqs=2 ** 22), SHAPE),
     (dict(scale=0.0), SHAPE), (dict(scale=-1.0), SHAPE), (dict(scale=float("inf")), SHAPE),
     (dict(scale=float("nan")), SHAPE),
@@ -106,7 +106,7 @@ PAGED = dict(dtype=BF16, q=P[0], q_stride=2048, cache_dtype=E4M3, k_cache=P[1], 
     (dict(dtype=F32, cache_dtype=BF16), DTYPE),
     (dict(kv_heads=5), SHAPE), (dict(heads=0), SHAPE), (dict(head_dim=80), SHAPE), (dict(n_seqs=-1), SHAPE),
     (dict(n_seqs=2 ** 20), SHAPE), (dict(n_pages=-1), SHAPE), (dict(max_pages=-1), SHAPE), (dict(page_size=0), SHAPE),
-    (dict(page_size=-64), SHAPE), (dict(n_pages=2 ** 30), SHAPE), (dict(max_pages=2 ** 30), SHAPE),
+    (dict(page_size=-64), SHAPE), (dict(n_pages=2 ** 30), SHAPE), (dict(max_pages=2 ** 24 + 1), SHAPE),
     (dict(page_size=2 ** 31 - 1), SHAPE), (dict(scale=0.0), SHAPE), (dict(scale=float("nan")), SHAPE),
     (dict(q_stride=1024), SHAPE), (dict(q_stride=2052), SHAPE), (dict(q=P[0] + 2), SHAPE), (dict(k_cache=P[1] + 8), SHAPE),
     (dict(o=P[7] + 8), SHAPE), (dict(lse=P[8] + 2), SHAPE), (dict(page_table=P[5] + 1), SHAPE),
@@ -129,7 +129,7 @@ def test_paged_workspace_bytes(lib):
     f = lib.hsa_paged_attention_workspace_bytes
     assert f(BF16, 1, 16, 2, 64, 2048) == 0                 # too short to split
     assert 0 < f(BF16, 1, 16, 2, 64, 7000) < f(BF16, 64, 16, 2, 64, 7000)
-    for args in [(BF16, 10000, 64, 8, 128, 2 ** 31 - 1), (F32, 1, 64, 64, 128, 2 ** 31 - 1), (BF16, 2, 1, 1, 64, 300)]:
+    for args in [(BF16, 10000, 64, 8, 128, 2 ** 30), (F32, 1, 64, 64, 128, 2 ** 30), (BF16, 2, 1, 1, 64, 300)]:
         assert f(*args) <= 32 << 20 == H.PAGED_WORKSPACE_BYTES
     for args in [(E4M3, 1, 16, 2, 64, 700), (BF16, -1, 16, 2, 64, 700), (BF16, 1, 16, 3, 64, 700),
                  (BF16, 1, 16, 2, 65, 700), (BF16, 1, 16, 2, 64, -1), (BF16, 1, 16, 2, 64, 2 ** 31)]:
