@@ -198,6 +198,8 @@ struct Attend {
     const float sl2e = a.scale * kLog2e;
     const int32_t* pages = a.page_table + (long)s * a.max_pages;
     bf16* vl = reinterpret_cast<bf16*>(sh.buf[wave]);
+    // V rows in LDS: chunk c of row r at slot c ^ f(r), so that the rows' writes and
+    // the transpose reads (16 rows, 2 chunks) spread over the banks
     auto swz = [](int r) { return DH == 128 ? (r & 7) << 1 : ((r >> 1) & 3) << 1; };
 
     // one block ahead: its rows (as held), exponents, and which of its keys exist;
@@ -520,17 +522,26 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a, P
   const int lane_p = threadIdx.x / C, c = (threadIdx.x - lane_p * C) * 4;
   float m = -INFINITY, l = 0.f;
   f32x4 sum = {};
-#pragma unroll 4
-  for (int i = lane_p; i <= note.more; i += G) {
-    const Part<DH>* p = parts + 2 * (long)(w0 + i) + (i ? 0 : note.slot);
-    const f32x2 ml = *reinterpret_cast<const f32x2*>(&p->ml[2 * r]);
-    const f32x4 x = *reinterpret_cast<const f32x4*>(&p->o[r * DH + c]);
-    if (ml[0] == -INFINITY && ml[1] == 0.f) continue;  // no key, or no finite score
-    const float m_new = fmaxf(m, ml[0]);
-    const float was = m == -INFINITY ? 0.f : rescale<F32>(m, m_new, a.scale), wt = rescale<F32>(ml[0], m_new, a.scale);
-    m = m_new;
-    l = fmaf(wt, ml[1], l * was);
-    sum = sum * was + wt * x;
+  constexpr int U = 4;  // parts loaded at once by each
+  for (int i0 = lane_p; i0 <= note.more; i0 += U * G) {
+    f32x2 ml[U];
+    f32x4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = min(i0 + u * G, note.more);
+      const Part<DH>* p = parts + 2 * (long)(w0 + i) + (i ? 0 : note.slot);
+      ml[u] = *reinterpret_cast<const f32x2*>(&p->ml[2 * r]);
+      x[u] = *reinterpret_cast<const f32x4*>(&p->o[r * DH + c]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i0 + u * G > note.more || (ml[u][0] == -INFINITY && ml[u][1] == 0.f)) continue;  // no key, or no finite score
+      const float m_new = fmaxf(m, ml[u][0]);
+      const float was = m == -INFINITY ? 0.f : rescale<F32>(m, m_new, a.scale), wt = rescale<F32>(ml[u][0], m_new, a.scale);
+      m = m_new;
+      l = fmaf(wt, ml[u][1], l * was);
+      sum = sum * was + wt * x[u];
+    }
   }
   sums[lane_p][c / 4] = sum;
   if (c == 0) {
