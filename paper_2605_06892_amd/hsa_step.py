@@ -427,114 +427,59 @@ def hsa_rope_table(theta: float, head_dim: int, grid) -> torch.Tensor:
 
 
 # Calls over several sequences. Their row inputs may be strided (slices of one projection's
-# output), and every tensor has to be on the current device. Their kernels take a few us for a
-# small batch, so each call tests everything in one expression of plain attributes (5 us of the former
-# checks, one function each, were 2) and names what is wrong only once something is.
+# output), and every tensor has to be on the current device. Their kernels take 3 us for a small
+# batch, so their marshalling and its checks are compiled (csrc/seq_binding.cpp): wrong devices, layouts and
+# shapes raise ValueError, wrong types TypeError, a refusal of the C entry point HsaStepError.
 
-_I32, _F8 = torch.int32, torch.float8_e4m3fn
+_seq = None
+
+
+def _binding():
+    global _seq
+    if _seq is None:
+        lib()  # says what to do if nothing was built
+        from . import _seq_binding
+        _seq = _seq_binding
+    return _seq
 
 
 def _here() -> int:
     try:
         return _device() if _device else torch.cuda.current_device()
     except RuntimeError:  # no device at all: the tensors are what the caller hears about
-        return -2
+        return -1
 
 
 def _stream_here(stream, dev: int):
     """The stream's handle: the current one of device dev, or a given one of that device."""
     if stream is None:
+        if dev < 0:
+            return None
         return _raw_stream(dev) if _raw_stream else torch.cuda.current_stream().cuda_stream
     if stream.device_index != dev:
         raise ValueError(f"the stream must be of the current device (cuda:{dev}), got {stream.device}")
     return stream.cuda_stream
 
 
-def _held(dev: int, *ts) -> bool:
-    """Contiguous tensors on the device."""
-    for t in ts:
-        if t.get_device() != dev or not t.is_contiguous():
-            return False
-    return True
-
-
-def _refuse(dev: int, rows, held, int32, width, message: str):
-    """Raise what is wrong with a call: rows (2-dimensional inputs with contiguous rows), held (contiguous tensors or
-    None), int32 (index tensors), width (a sequence of (what, is fine) pairs of types, then shapes)."""
-    for t in (*rows, *held):
-        if t is not None and not t.is_cuda:
-            raise ValueError("tensors must be device tensors")
-        if t is not None and t.get_device() != dev:
-            raise ValueError(f"tensors must be on the current device (cuda:{dev}), got {t.device}")
-    for t in rows:
-        if t.dim() != 2 or t.stride(1) != 1:
-            raise ValueError("rows must be 2-dimensional with contiguous values")
-    for t in held:
-        if t is not None and not t.is_contiguous():
-            raise ValueError("tensors must be contiguous")
-    for t in int32:
-        if t.dtype != _I32:
-            raise TypeError("indices, offsets, pages and lengths are int32")
-    for what, fine in width:
-        if not fine:
-            raise TypeError(what)
-    raise ValueError(message)
-
-
-def _caches_fit(dt, kc, vc, ke, ve, kv_heads: int) -> bool:
-    """Caches of rows' dtype dt, or of codes with their exponents (device and layout apart)."""
-    cd, shape = kc.dtype, kc.shape
-    if cd is not vc.dtype or shape != vc.shape or len(shape) != 2:
-        return False
-    if cd is not _F8:
-        return cd is dt
-    if ke is None or ve is None or ke.dtype is not torch.int8 or ve.dtype is not torch.int8:
-        return False
-    want = (shape[0], kv_heads)
-    return ke.shape == want and ve.shape == want
-
-
-_CACHES = "caches hold the rows' dtype, or float8_e4m3fn with int8 exponents [n_rows, kv_heads], and match each other"
-
-
-def _cache_call(name: str, k, v, idx, n: int, kv_heads: int, kc, vc, ke, ve, stream) -> None:
-    dev = _here()
-    dt, kst, vst, ksh, vsh, csh = k.dtype, k.stride(), v.stride(), k.shape, v.shape, kc.shape
-    e4m3 = kc.dtype is _F8
-    if not (len(kst) == 2 == len(vst) and kst[1] == 1 == vst[1] and dt is v.dtype and dt in _DTYPES
-            and idx.dtype is _I32 and _caches_fit(dt, kc, vc, ke, ve, kv_heads) and ksh[1] == csh[1] == vsh[1]
-            and kv_heads > 0 and csh[1] % kv_heads == 0 and ksh[0] >= n <= vsh[0] and n <= idx.numel()
-            and k.get_device() == dev == v.get_device() and _held(dev, idx, kc, vc)
-            and (not e4m3 or _held(dev, ke, ve))):
-        _refuse(dev, (k, v), (idx, kc, vc, ke, ve), (idx,),
-                (("rows are bf16 or fp32, the same for k and v", dt is v.dtype and dt in _DTYPES),
-                 (_CACHES, _caches_fit(dt, kc, vc, ke, ve, kv_heads))),
-                "k and v must hold n rows of the caches' width, a multiple of kv_heads, and idx n indices")
-    dt = _DTYPES[dt]
-    rows = (k.data_ptr(), kst[0] if ksh[0] > 1 else ksh[1], v.data_ptr(), vst[0] if vsh[0] > 1 else vsh[1])
-    kep, vep = (ke.data_ptr(), ve.data_ptr()) if e4m3 else (None, None)
-    stream = _stream_here(stream, dev)
-    if name == "hsa_cache_store":
-        st = lib().hsa_cache_store(dt, *rows, idx.data_ptr(), n, csh[0], kv_heads, csh[1] // kv_heads,
-                                   E4M3 if e4m3 else dt, kc.data_ptr(), vc.data_ptr(), kep, vep, stream)
-    else:
-        st = lib().hsa_cache_load(E4M3 if e4m3 else dt, kc.data_ptr(), vc.data_ptr(), kep, vep, idx.data_ptr(), n, csh[0],
-                                  kv_heads, csh[1] // kv_heads, dt, *rows, stream)
-    if st:
-        raise HsaStepError(name, st)
-
-
 def hsa_cache_store(k, v, idx, n: int, kv_heads: int, k_cache, v_cache, k_exp=None, v_exp=None, stream=None) -> None:
     """k_cache[idx[:n]] = k[:n] and the same for v, quantized on the way into
     float8_e4m3fn caches (k_exp, v_exp: their int8 exponents [n_rows, kv_heads]);
     an index outside the cache skips its row."""
-    _cache_call("hsa_cache_store", k, v, idx, n, kv_heads, k_cache, v_cache, k_exp, v_exp, stream)
+    dev = _here()
+    st = (_seq or _binding()).cache_store(dev, _stream_here(stream, dev), k, v, idx, n, kv_heads, k_cache, v_cache, k_exp,
+                                          v_exp)
+    if st:
+        raise HsaStepError("hsa_cache_store", st)
 
 
 def hsa_cache_load(k_cache, v_cache, idx, n: int, kv_heads: int, k, v, k_exp=None, v_exp=None, stream=None) -> None:
     """k[:n] = k_cache[idx[:n]] and the same for v, as values of k's dtype;
     zeros for an index outside the cache."""
-    _cache_call("hsa_cache_load", k, v, idx, n, kv_heads, k_cache, v_cache, k_exp, v_exp, stream)
+    dev = _here()
+    st = (_seq or _binding()).cache_load(dev, _stream_here(stream, dev), k, v, idx, n, kv_heads, k_cache, v_cache, k_exp,
+                                         v_exp)
+    if st:
+        raise HsaStepError("hsa_cache_load", st)
 
 
 def hsa_packed_attention(q, k, v, cu_q, cu_kv, heads: int, kv_heads: int, head_dim: int, scale: float, causal: bool,
@@ -543,25 +488,8 @@ def hsa_packed_attention(q, k, v, cu_q, cu_kv, heads: int, kv_heads: int, head_d
     bottom-right aligned where causal; o and lse (log of the softmax sums,
     fp32 [n_q, heads]) outside every sequence are left as they were."""
     dev = _here()
-    dt, qsh, ksh = q.dtype, q.shape, k.shape
-    qst, kst, vst = q.stride(), k.stride(), v.stride()
-    n_seqs = cu_q.numel() - 1
-    if not (len(qst) == len(kst) == len(vst) == 2 and qst[1] == kst[1] == vst[1] == 1
-            and dt is k.dtype and dt is v.dtype and dt is o.dtype and dt in _DTYPES
-            and cu_q.dtype is _I32 and cu_kv.dtype is _I32 and cu_kv.numel() == n_seqs + 1 > 0
-            and qsh[1] == heads * head_dim and o.shape == qsh and ksh[1] == kv_heads * head_dim and v.shape == ksh
-            and q.get_device() == dev == k.get_device() and v.get_device() == dev and _held(dev, cu_q, cu_kv, o)
-            and (lse is None or (lse.dtype is torch.float32 and lse.shape == (qsh[0], heads) and _held(dev, lse)))):
-        _refuse(dev, (q, k, v), (cu_q, cu_kv, o, lse), (cu_q, cu_kv),
-                (("q, k, v and o are bf16 or fp32, all the same", dt is k.dtype is v.dtype is o.dtype and dt in _DTYPES),
-                 ("lse is fp32 [n_q, heads]", lse is None or (lse.dtype is torch.float32 and lse.shape == (qsh[0], heads)))),
-                "q and o are [n_q, heads * head_dim], k and v [n_kv, kv_heads * head_dim], cu_q and cu_kv [n_seqs + 1]")
-    n_q, n_kv = qsh[0], ksh[0]
-    st = lib().hsa_packed_attention(_DTYPES[dt], q.data_ptr(), qst[0] if n_q > 1 else qsh[1], k.data_ptr(),
-                                    kst[0] if n_kv > 1 else ksh[1], v.data_ptr(), vst[0] if n_kv > 1 else ksh[1],
-                                    cu_q.data_ptr(), cu_kv.data_ptr(), n_seqs, n_q, n_kv, heads, kv_heads, head_dim, scale,
-                                    1 if causal else 0, o.data_ptr(), None if lse is None else lse.data_ptr(),
-                                    _stream_here(stream, dev))
+    st = (_seq or _binding()).packed_attention(dev, _stream_here(stream, dev), q, k, v, cu_q, cu_kv, heads, kv_heads,
+                                               head_dim, scale, causal, o, lse)
     if st:
         raise HsaStepError("hsa_packed_attention", st)
 
@@ -581,31 +509,8 @@ def hsa_paged_attention(q, k_cache, v_cache, page_table, kv_lens, page_size: int
     heads, kv_heads, head_dim, page_table.shape[1] * page_size) bytes (None where that is
     0), or PAGED_WORKSPACE_BYTES for any call."""
     dev = _here()
-    dt, qsh, qst, psh, csh = q.dtype, q.shape, q.stride(), page_table.shape, k_cache.shape
-    e4m3 = k_cache.dtype is _F8
-    if not (len(qst) == 2 and qst[1] == 1 and dt is o.dtype and dt in _DTYPES and o.shape == qsh
-            and _caches_fit(dt, k_cache, v_cache, k_exp, v_exp, kv_heads) and csh[1] == kv_heads * head_dim
-            and qsh[1] == heads * head_dim and page_table.dtype is _I32 and kv_lens.dtype is _I32
-            and len(psh) == 2 and psh[0] == qsh[0] == kv_lens.numel() and page_size > 0
-            and q.get_device() == dev and _held(dev, k_cache, v_cache, page_table, kv_lens, o)
-            and (workspace is None or _held(dev, workspace)) and (not e4m3 or _held(dev, k_exp, v_exp))
-            and (lse is None or (lse.dtype is torch.float32 and lse.shape == (qsh[0], heads) and _held(dev, lse)))):
-        _refuse(dev, (q,), (k_cache, v_cache, page_table, kv_lens, o, workspace, k_exp, v_exp, lse), (page_table, kv_lens),
-                (("q and o are bf16 or fp32, the same", dt is o.dtype and dt in _DTYPES),
-                 (_CACHES, _caches_fit(dt, k_cache, v_cache, k_exp, v_exp, kv_heads)),
-                 ("lse is fp32 [n_seqs, heads]",
-                  lse is None or (lse.dtype is torch.float32 and lse.shape == (qsh[0], heads)))),
-                "q and o are [n_seqs, heads * head_dim], the caches [n_rows, kv_heads * head_dim], page_table "
-                "[n_seqs, max_pages], kv_lens [n_seqs], page_size at least 1")
-    kep, vep = (k_exp.data_ptr(), v_exp.data_ptr()) if e4m3 else (None, None)
-    st = lib().hsa_paged_attention(_DTYPES[dt], q.data_ptr(), qst[0] if qsh[0] > 1 else qsh[1],
-                                   E4M3 if e4m3 else _DTYPES[dt], k_cache.data_ptr(), v_cache.data_ptr(), kep, vep,
-                                   page_table.data_ptr(), psh[1], kv_lens.data_ptr(), qsh[0], csh[0] // page_size,
-                                   page_size, heads, kv_heads, head_dim, scale, o.data_ptr(),
-                                   None if lse is None else lse.data_ptr(),
-                                   None if workspace is None else workspace.data_ptr(),
-                                   0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                   _stream_here(stream, dev))
+    st = (_seq or _binding()).paged_attention(dev, _stream_here(stream, dev), q, k_cache, v_cache, page_table, kv_lens,
+                                              page_size, heads, kv_heads, head_dim, scale, o, workspace, k_exp, v_exp, lse)
     if st:
         raise HsaStepError("hsa_paged_attention", st)
 
