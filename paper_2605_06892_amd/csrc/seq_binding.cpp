@@ -65,6 +65,13 @@ struct Args {
   }
 };
 
+// The interpreter is free while a call enqueues, as it is in a ctypes call: a full
+// queue may make it wait.
+struct Unlocked {
+  PyThreadState* state = PyEval_SaveThread();
+  ~Unlocked() { PyEval_RestoreThread(state); }
+};
+
 struct Here {
   int64_t device;
   void on(const at::Tensor& t) const {
@@ -157,6 +164,7 @@ int cache(Args& a, bool store) {
       n > v.size(0) || n > idx.numel())
     value_error("k and v must hold n rows of the caches' width, a multiple of kv_heads, and idx n indices");
   const int32_t head_dim = (int32_t)(c.width / kv_heads);
+  const Unlocked unlocked;
   if (store)
     return hsa_cache_store(dt, k.data_ptr(), row_stride(k), v.data_ptr(), row_stride(v), ints(idx), n, c.n_rows, kv_heads,
                            head_dim, c.dtype, kc.data_ptr(), vc.data_ptr(), const_cast<int8_t*>(bytes(c.k_exp)),
@@ -191,6 +199,7 @@ int packed(Args& a) {
       q.size(1) != (int64_t)heads * head_dim || o.sizes() != q.sizes() || k.size(1) != (int64_t)kv_heads * head_dim ||
       v.sizes() != k.sizes())
     value_error("q and o are [n_q, heads * head_dim], k and v [n_kv, kv_heads * head_dim], cu_q and cu_kv [n_seqs + 1]");
+  const Unlocked unlocked;
   return hsa_packed_attention(dt, q.data_ptr(), row_stride(q), k.data_ptr(), row_stride(k), v.data_ptr(), row_stride(v),
                               ints(cu_q), ints(cu_kv), (int32_t)(cu_q.numel() - 1), q.size(0), k.size(0), heads, kv_heads,
                               head_dim, scale, causal, o.data_ptr(), l, stream);
@@ -221,6 +230,7 @@ int paged(Args& a) {
       o.sizes() != q.sizes() || c.width != (int64_t)kv_heads * head_dim || c.n_rows / page_size > INT32_MAX)
     value_error("q and o are [n_seqs, heads * head_dim], the caches [n_rows, kv_heads * head_dim], page_table "
                 "[n_seqs, max_pages], kv_lens [n_seqs], page_size at least 1");
+  const Unlocked unlocked;
   return hsa_paged_attention(dt, q.data_ptr(), row_stride(q), c.dtype, kc.data_ptr(), vc.data_ptr(), bytes(c.k_exp),
                              bytes(c.v_exp), ints(table), (int32_t)table.size(1), ints(lens), (int32_t)q.size(0),
                              (int32_t)(c.n_rows / page_size), page_size, heads, kv_heads, head_dim, scale, o.data_ptr(), l,
@@ -231,7 +241,8 @@ template <class F>
 PyObject* call(PyObject* const* at, Py_ssize_t n, F f) {
   try {
     Args a{at, n};
-    return PyLong_FromLong(f(a));
+    const int status = f(a);
+    return PyLong_FromLong(status);
   } catch (const Refusal& r) {
     PyErr_SetString(r.type, r.what.c_str());
   } catch (const std::exception& e) {

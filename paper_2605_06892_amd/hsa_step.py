@@ -3,8 +3,9 @@
 Argument marshalling only: every function takes torch tensors (device memory
 from PyTorch-ROCm) and scalars, passes raw pointers and the current HIP stream
 to the C entry point of the same name, and raises HsaStepError on a non-zero
-status. No computation happens here; there is no fallback path. Importing this
-module fails if the HIP library has not been built.
+status. The calls over several sequences go through a compiled module instead of
+ctypes (csrc/seq_binding.cpp). No computation happens here; there is no fallback
+path. The first call fails if the HIP library has not been built.
 """
 
 from __future__ import annotations
