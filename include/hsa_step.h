@@ -632,7 +632,8 @@ int hsa_packed_attention(int dtype, const void* q, int64_t q_stride, const void*
 #define HSA_STEP_PAGED_WORKSPACE_BYTES (32u << 20)
 
 /* Workspace bytes hsa_paged_attention needs, at most
- * HSA_STEP_PAGED_WORKSPACE_BYTES. 0 where it needs none, and for invalid sizes. */
+ * HSA_STEP_PAGED_WORKSPACE_BYTES, and enough for fewer sequences and rows too. 0 where
+ * it needs none, and for invalid sizes. */
 size_t hsa_paged_attention_workspace_bytes(int dtype, int32_t n_seqs, int32_t heads,
                                            int32_t kv_heads, int32_t head_dim, int64_t max_len);
 

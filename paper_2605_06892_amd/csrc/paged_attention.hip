@@ -3,7 +3,7 @@
 // all the query heads of its group, and that reading bounds it.
 //
 // Work split. An item is (sequence, key/value head, 16 query heads of its group). Where no
-// sequence can be longer than kWholeLen rows, an item is a workgroup of 8 waves. Longer
+// sequence can be longer than whole_len() rows, an item is a workgroup of 8 waves. Longer
 // ones come in tiles of 128 rows: all tiles of all items, in order, are dealt to the
 // workgroups (of 4 waves) in equal runs, so that a batch of very different lengths
 // loads the CUs evenly and one long sequence is spread over all of them. A run that holds a
@@ -567,9 +567,22 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a, P
 
 int gts_of(int group) { return (group + kRows - 1) / kRows; }
 
-// Rows up to which an item is one workgroup's.
-constexpr long kWholeLen = 2048;
-bool splits(long max_len) { return max_len > kWholeLen; }
+// Rows up to which an item is one workgroup's. Dealing out tiles costs the walk and the join
+// (4 to 5 us), a whole item the time of its rows in one workgroup, and the fewer items, the
+// fewer CUs share that. Whole and dealt, us, bf16, 128 channels, batches of half to full length:
+//     8 items    700 rows 11.1  9.8    1000 14.6  9.7    1500 19.9 10.1
+//    64          700      11.8 11.8    1000 15.7 12.6    1500 21.3 16.2
+//   128         1000      16.7 19.1    1250 19.4 19.3    2000 28.0 25.4
+//   256         1000      20.6 26.0    2000 35.7 38.3    4000 73.5 75.4
+// (64 channels and e4m3 cross within a third of these.)
+constexpr long kLeastWhole = 768;
+long whole_len(long items) {
+  const int cus = compute_units();
+  return items * 4 <= cus ? kLeastWhole : items * 2 <= cus ? 1024 : 2048;
+}
+bool splits(int n_seqs, int kv_heads, int group, long max_len) {
+  return max_len > whole_len((long)n_seqs * kv_heads * gts_of(group));
+}
 
 // Workgroups the tiles are dealt to: as many as run at once, no more than tiles
 // if every sequence is as long as it may be.
@@ -582,7 +595,7 @@ template <bool F32, bool E4M3, int DH, bool ALIGNED>
 hipError_t launch(const PagedArgs& a, hipStream_t s) {
   const long max_len = (long)a.max_pages * a.page_size;
   Plan plan{0, gts_of(a.group), FastDiv((uint32_t)a.page_size)};
-  if (!splits(max_len)) {
+  if (!splits(a.n_seqs, a.kv_heads, a.group, max_len)) {
     hipLaunchKernelGGL((paged_whole_kernel<F32, E4M3, DH, ALIGNED>), dim3((unsigned)(a.n_seqs * a.kv_heads * plan.gts)),
                        dim3(kWholeWaves * 64), 0, s, a, plan);
     return hipGetLastError();
@@ -604,8 +617,10 @@ hipError_t launch_held(const PagedArgs& a, bool e4m3, hipStream_t s) {
 
 }  // namespace
 
+// Asked for as if every item were dealt from kLeastWhole rows on, so that a workspace
+// made for n_seqs and max_len serves fewer sequences too.
 size_t paged_attention_bytes(int n_seqs, int kv_heads, int group, int head_dim, long max_len) {
-  if (n_seqs <= 0 || !splits(max_len)) return 0;
+  if (n_seqs <= 0 || max_len <= kLeastWhole) return 0;
   return (size_t)workgroups(n_seqs, kv_heads, group, max_len) * (2 * kRows * (head_dim + 2) * sizeof(float) + sizeof(Note));
 }
 

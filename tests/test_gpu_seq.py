@@ -574,7 +574,7 @@ PAGED = [
 @pytest.mark.parametrize("wide", [False, True])
 @pytest.mark.parametrize("dtype,cache", [("bf16", "bf16"), ("bf16", "e4m3"), ("f32", "f32"), ("f32", "e4m3")])
 def test_paged(dtype, cache, wide, dh, lens, page, heads, kv):
-    """wide: page tables of over 2048 rows, whose launch deals tiles of rows to the workgroups and joins the parts."""
+    """wide: page tables of 5000 rows, whose launch deals tiles of rows to the workgroups and joins the parts."""
     q, k, v, held, table = paged_inputs(sum(lens) + page, dtype, cache, lens, page, heads, kv, dh,
                                         max_pages=5000 // page if wide else None)
     scale = dh ** -0.5
@@ -598,6 +598,23 @@ def test_paged_many_sequences_and_one_long(dtype, cache, page):
     o, lse = run_paged(q, held, table, lens, page, 4, 2, 64, 0.125)
     want, lw, A, S = paged_want(q, k, v, table, lens, page, k.shape[0] // page, 4, 2, 64, 0.125)
     check(o, lse, want, lw, A, S, dtype, 9000, 64)
+
+
+@pytest.mark.parametrize("n_seqs,kv,rows", [(n, kv, r) for n, kv in ((1, 1), (16, 4), (13, 5), (32, 4), (43, 3))
+                                             for r in (768, 776, 1024, 1032, 2048, 2056)])
+def test_paged_table_lengths_where_the_split_changes(n_seqs, kv, rows):
+    """Tables just up to and just past each length at which a launch goes over from whole items to dealt tiles,
+    in a workspace of exactly the bytes asked for."""
+    lens = [rows] + [(i * 613) % (rows + 1) for i in range(1, n_seqs)]
+    q, k, v, held, table = paged_inputs(6, "bf16", "bf16", lens, 8, 2 * kv, kv, 64, max_pages=rows // 8)
+    nb = H.hsa_paged_attention_workspace_bytes(torch.bfloat16, n_seqs, 2 * kv, kv, 64, rows)
+    o, ws = Guarded(q.shape, torch.bfloat16, 1), Guarded((max(nb, 1),), torch.uint8, 2)
+    ws.t.fill_(255)
+    _, lse = run_paged(q, held, table, lens, 8, 2 * kv, kv, 64, 0.125, o.t, ws.t)
+    want, lw, A, S = paged_want(q, k, v, table, lens, 8, k.shape[0] // 8, 2 * kv, kv, 64, 0.125)
+    check(o.t, lse, want, lw, A, S, "bf16", rows, 64)
+    o.check("o")
+    ws.check("workspace")
 
 
 @pytest.mark.parametrize("cache", ["bf16", "e4m3"])

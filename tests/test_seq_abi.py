@@ -127,7 +127,10 @@ def test_paged_of_nothing(lib):
 
 def test_paged_workspace_bytes(lib):
     f = lib.hsa_paged_attention_workspace_bytes
-    assert f(BF16, 1, 16, 2, 64, 2048) == 0                 # too short to split
+    assert f(BF16, 1, 16, 2, 64, 768) == 0                  # too short to split
+    for rows in (769, 1025, 2048, 2049, 7000):              # enough for fewer sequences and rows
+        need = [f(BF16, n, 16, 2, 64, rows) for n in range(300)]
+        assert need == sorted(need) and all(need[1:]) and f(BF16, 40, 16, 2, 64, rows - 1) <= need[40]
     assert 0 < f(BF16, 1, 16, 2, 64, 7000) < f(BF16, 64, 16, 2, 64, 7000)
     for args in [(BF16, 10000, 64, 8, 128, 2 ** 30), (F32, 1, 64, 64, 128, 2 ** 30), (BF16, 2, 1, 1, 64, 300)]:
         assert f(*args) <= 32 << 20 == H.PAGED_WORKSPACE_BYTES
