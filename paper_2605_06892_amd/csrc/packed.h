@@ -150,7 +150,7 @@ __device__ __forceinline__ void add_odd(f32x4& sum, const bf16* v, long stride, 
     }
 }
 
-// bf16, 256 rows per workgroup (packed_attention_large.hip)
+// bf16, 128 or 256 rows per workgroup, for 64- and 128-wide heads (packed_attention_large.hip)
 hipError_t launch_packed_attention_large(const PackedArgs& a, int head_dim, hipStream_t s);
 // Estimated time of a launch with tiles of `rows` rows and workgroups of `waves` waves (us,
 // MI355X), from the means of the batch's lengths, which are all the host knows: a fixed

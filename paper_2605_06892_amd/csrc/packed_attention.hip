@@ -264,26 +264,31 @@ hipError_t launch_small(const PackedArgs& a, hipStream_t s) {
 }
 
 // Fitted to 499 launches of 1, 5 and 20 prompts of 1 to 4500 tokens, with and without 1000
-// rows before them, 1 to 40 heads of either width: the least estimate takes 1.2% more
-// than the fastest of the five on average, over 10% more in one launch of 38. Measured, 128-wide
-// heads, in this order: 8 heads, no mask, 1 prompt of 400 tokens 10.2, 10.2, 11.8, 12.2 and 15.8;
-// of 1000 29.2, 26.8, 19.0, 18.6 and 28.6; of 4500 395, 366, 241, 247 and 103; causal, 20 prompts
-// of 25 to 77 15.1, 10.6, 12.1, 13.1 and 10.0.
-constexpr PackedCost kCosts[2][5] = {{{16, 8, 2.6, 2.2, 0.130, 0.144},   // 64-wide heads
-                                      {16, 4, 3.9, 0.85, 0.145, 0.05},
-                                      {32, 8, 0.0, 5.1, 0.169, 0.021},
-                                      {32, 4, 2.7, 2.5, 0.161, 0.202},
-                                      {256, 8, 0.0, 6.9, 0.490, 0.244}},
-                                     {{16, 8, 0.0, 5.2, 0.291, 0.05},    // 128-wide
-                                      {16, 4, 3.2, 2.4, 0.272, 0.116},
-                                      {32, 8, 0.0, 6.2, 0.353, 0.175},
-                                      {32, 4, 0.0, 6.6, 0.340, 0.292},
-                                      {256, 8, 0.0, 8.2, 0.713, 0.05}}};
+// rows before them, 1 to 40 heads of either width: the least estimate takes 1.8% more
+// than the fastest of the five on average, over 10% more in one launch of 19. Measured, us, in this
+// order, no mask but for 20 prompts:
+//   128-wide, 8 heads      1 prompt of 400 tokens   9.6    9.4   11.0   11.2   15.2
+//                          1 of 1000               28.5   26.3   18.6   18.1   28.2
+//                          1 of 4500                392    365    238    250    104
+//                          20 of 25 to 77          14.4   10.5   12.2   13.1    8.6
+//   64-wide, 32/8 heads    1 of 400                14.7   13.1   13.1   10.4    9.5
+//                          1 of 1000               44.8   42.8   38.2   30.0   18.0
+//                          20 of 25 to 77          19.4   11.2   19.7   12.0    8.4
+constexpr PackedCost kCosts[2][5] = {{{16, 8, 2.5, 2.0, 0.132, 0.060},   // 64-wide heads
+                                      {16, 4, 3.5, 0.87, 0.144, 0.050},
+                                      {32, 8, 0.0, 4.8, 0.167, 0.067},
+                                      {32, 4, 2.7, 2.3, 0.164, 0.207},
+                                      {128, 4, 2.9, 3.0, 0.283, 0.357}},
+                                     {{16, 8, 0.0, 5.0, 0.293, 0.136},   // 128-wide
+                                      {16, 4, 3.0, 2.3, 0.274, 0.134},
+                                      {32, 8, 0.0, 6.0, 0.351, 0.174},
+                                      {32, 4, 0.0, 6.3, 0.351, 0.316},
+                                      {256, 8, 0.0, 7.6, 0.719, 0.050}}};
 
 template <int DH>
 hipError_t launch_dh(const PackedArgs& a, hipStream_t s) {
   const PackedCost c = packed_choice(a, kCosts[DH == 128]);
-  if (c.rows == 256) return launch_packed_attention_large(a, DH, s);
+  if (c.rows >= 128) return launch_packed_attention_large(a, DH, s);
   if (c.rows == 32) return c.waves == 8 ? launch_small<DH, 32, 8>(a, s) : launch_small<DH, 32, 4>(a, s);
   return c.waves == 8 ? launch_small<DH, 16, 8>(a, s) : launch_small<DH, 16, 4>(a, s);
 }

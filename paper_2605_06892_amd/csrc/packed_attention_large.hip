@@ -1,8 +1,8 @@
-// bf16 attention of packed sequences: 256 rows of one key/value head per
-// workgroup (rows are (query, head of the group) pairs, see packed.h).
+// bf16 attention of packed sequences: 256 rows of one 128-wide key/value head per
+// workgroup, 128 of a 64-wide one (rows are (query, head of the group) pairs, see packed.h).
 //
-// 8 waves of 32 rows. K/V tiles of 96 keys go global -> LDS directly, three tiles deep
-// (144 KB of LDS at 128-wide heads), issued two tiles ahead by one wave per SIMD,
+// 8 or 4 waves of 32 rows. K/V tiles of 96 keys go global -> LDS directly, three tiles deep
+// (144 or 72 KB of LDS), issued two tiles ahead by one wave per SIMD,
 // one barrier per tile. LDS rows are unpadded, their 16-byte chunks permuted by an XOR with
 // a function of the row, so that the K fragment reads (16 rows, one chunk) and the V
 // transpose reads (4 rows, 4 chunks) hit disjoint banks. Per 32-key block and wave:
@@ -26,8 +26,6 @@
 namespace hsa {
 namespace {
 
-constexpr int NW = 8;                   // waves
-constexpr int BQ = NW * 32;             // rows per workgroup
 constexpr int BKV = 96;                 // keys per LDS tile (three 32-key blocks)
 constexpr int NBUF = 3;                 // LDS tiles in flight
 constexpr float kSlowSum = 65536.0f;    // 2^16: raise the reference maximum
@@ -49,8 +47,17 @@ __device__ __forceinline__ int swz_v(int r) {
   return DH == 128 ? ((r & 3) << 2) : (((r >> 1) & 1) << 2);
 }
 
+// Waves of a workgroup. At 64-wide heads LDS holds two workgroups of 4 waves per CU, which start and
+// end apart from each other: as fast as one of 8 on long prompts (32/8 heads, 8000 causal
+// tokens 281 and 277 us), faster where tiles are few (1000 tokens 17 and 21). At 128 it holds one, and
+// a wave alone on its SIMD takes as long for a block as each of two: 1000 tokens 31 and 28 us, 3000
+// 138 and 81.
 template <int DH>
-__global__ __launch_bounds__(NW * 64) void packed_large_kernel(PackedArgs a, PackedGrid grid) {
+constexpr int waves = DH == 64 ? 4 : 8;
+
+template <int DH>
+__global__ __launch_bounds__(waves<DH> * 64, 2) void packed_large_kernel(PackedArgs a, PackedGrid grid) {
+  constexpr int NW = waves<DH>, BQ = NW * 32;
   constexpr int CPR = DH / 8;        // 16-byte chunks per key row
   constexpr int RPS = 64 / CPR;      // rows per 1 KB LDS segment
   constexpr int SEGS = BKV / RPS;    // segments per tile
@@ -107,7 +114,7 @@ __global__ __launch_bounds__(NW * 64) void packed_large_kernel(PackedArgs a, Pac
   // this lane's part of a tile load: segment seg = i*LW + wave, row seg*RPS + lane/CPR,
   // LDS slot lane%CPR holding global chunk slot ^ f(row). Loads come from waves
   // 0..3 only, one per SIMD: a wave stalls while its loads issue, and the other
-  // wave of its SIMD keeps the matrix pipe busy meanwhile.
+  // wave of its SIMD, where there is one, keeps the matrix pipe busy meanwhile.
   const bf16* kg = static_cast<const bf16*>(a.k) + (long)t.k0 * a.k_stride + (long)h * DH;
   const bf16* vg = static_cast<const bf16*>(a.v) + (long)t.k0 * a.v_stride + (long)h * DH;
   constexpr int LW = 4;                 // loader waves
@@ -387,9 +394,9 @@ __global__ __launch_bounds__(NW * 64) void packed_large_kernel(PackedArgs a, Pac
 
 template <int DH>
 hipError_t launch(const PackedArgs& a, hipStream_t s) {
-  const PackedGrid g = packed_grid(a, BQ, DH * 2);
+  const PackedGrid g = packed_grid(a, waves<DH> * 32, DH * 2);
   if (g.groups < 0) return hipErrorInvalidValue;
-  hipLaunchKernelGGL((packed_large_kernel<DH>), dim3((unsigned)g.groups), dim3(NW * 64), 0, s, a, g);
+  hipLaunchKernelGGL((packed_large_kernel<DH>), dim3((unsigned)g.groups), dim3(waves<DH> * 64), 0, s, a, g);
   return hipGetLastError();
 }
 

@@ -72,7 +72,7 @@ def check(got, lse_got, want, lse_want, A, S, dtype, n_keys, dh):
 
 
 @pytest.fixture(params=[("bf16", ""), ("bf16", "16x8"), ("bf16", "16x4"), ("bf16", "32x8"), ("bf16", "32x4"),
-                        ("bf16", "256x8"), ("f32", "16x8"), ("f32", "16x4")],
+                        ("bf16", "128x4"), ("bf16", "256x8"), ("f32", "16x8"), ("f32", "16x4")],
                 ids=lambda p: "-".join(filter(None, p)))
 def form(request, monkeypatch):
     """The dtype, with every tile (rows x waves) whatever the launch would choose."""
