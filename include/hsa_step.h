@@ -644,9 +644,9 @@ size_t hsa_paged_attention_workspace_bytes(int dtype, int32_t n_seqs, int32_t he
  * of the caches, and
  *   o[s, h]   = sum_t softmax_t(scale <q[s, h], k[t, h / G]>) v[t, h / G]
  *   lse[s, h] = log sum_t exp(scale <q[s, h], k[t, h / G]>)
- * The cached rows are split over the workgroups whatever the lengths, and
- * the parts joined by a second kernel (an exact rearrangement of the softmax
- * sum). A sequence of length 0 has o = 0 and lse = -infinity. Rows in a page
+ * Behind long page tables the cached rows are split over the workgroups
+ * whatever the lengths, and the parts joined by a second kernel (an exact
+ * rearrangement of the softmax sum). A sequence of length 0 has o = 0 and lse = -infinity. Rows in a page
  * outside [0, n_pages) are left out of the sums; page table entries past a
  * sequence's length are not read.
  *   q            [n_seqs, heads * head_dim] dtype, rows q_stride elements apart
