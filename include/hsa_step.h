@@ -648,7 +648,8 @@ size_t hsa_paged_attention_workspace_bytes(int dtype, int32_t n_seqs, int32_t he
  * whatever the lengths, and the parts joined by a second kernel (an exact
  * rearrangement of the softmax sum). A sequence of length 0 has o = 0 and lse = -infinity. Rows in a page
  * outside [0, n_pages) are left out of the sums; page table entries past a
- * sequence's length are not read.
+ * sequence's length are not read. Rows of the caches that no sequence has may
+ * hold anything, exponents that were never written among it.
  *   q            [n_seqs, heads * head_dim] dtype, rows q_stride elements apart
  *   k_cache, ... as for hsa_cache_store, with n_pages * page_size rows
  *   page_table   int32 [n_seqs, max_pages]; pages may be shared by sequences

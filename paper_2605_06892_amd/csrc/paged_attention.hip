@@ -341,9 +341,11 @@ struct Attend {
           const int f = i * 64 + lane, r = f / CPR;
           u32x4 x;
           __builtin_memcpy(&x, &vr[i], CB);
-          if (cut && !(keys >> r & 1)) x = (u32x4){};  // 0 * infinity, as above
+          const bool gone = cut && !(keys >> r & 1);
+          if (gone) x = (u32x4){};  // 0 * infinity, as above
           if constexpr (E4M3) {
-            const float sv = pow2(ve[i]);
+            // an exponent that was never written may be -128, as a scale a NaN that makes one of 0 too
+            const float sv = pow2(gone ? 0 : ve[i]);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
               *reinterpret_cast<bf16x8*>(vl + r * DH + ((((f % CPR) * 2 + j) ^ swz(r)) * 8)) = widen(x[2 * j], x[2 * j + 1], sv);
