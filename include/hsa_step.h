@@ -609,7 +609,10 @@ int hsa_cache_load(int cache_dtype, const void* k_cache, const void* v_cache, co
  *   o[i, h]   = sum_j softmax_j(scale <q[i, h], k[j, h / G]>) v[j, h / G]
  *   lse[i, h] = log sum_j exp(scale <q[i, h], k[j, h / G]>)
  * A query that sees no key, or only keys whose score is -infinity, has o = 0
- * and lse = -infinity.
+ * and lse = -infinity whatever the values hold. In any other a value that is not
+ * finite makes its channel of o infinite or NaN where the key is seen with a
+ * positive weight; where that weight is 0 (a score of -infinity, or one so far
+ * below the greatest that its exponential is 0) the channel is unspecified.
  *   q           [n_q, heads * head_dim] dtype, rows q_stride elements apart
  *   k, v        [n_kv, kv_heads * head_dim] dtype, rows k_stride, v_stride apart
  *   cu_q, cu_kv int32 [n_seqs + 1] on the device, ascending, in [0, n_q] and
@@ -646,7 +649,8 @@ size_t hsa_paged_attention_workspace_bytes(int dtype, int32_t n_seqs, int32_t he
  *   lse[s, h] = log sum_t exp(scale <q[s, h], k[t, h / G]>)
  * Behind long page tables the cached rows are split over the workgroups
  * whatever the lengths, and the parts joined by a second kernel (an exact
- * rearrangement of the softmax sum). A sequence of length 0 has o = 0 and lse = -infinity. Rows in a page
+ * rearrangement of the softmax sum). A sequence of length 0, or with scores of
+ * -infinity only, has o = 0 and lse = -infinity. Rows in a page
  * outside [0, n_pages) are left out of the sums; page table entries past a
  * sequence's length are not read. Rows of the caches that no sequence has may
  * hold anything, exponents that were never written among it.

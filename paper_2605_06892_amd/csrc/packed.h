@@ -140,7 +140,7 @@ __device__ __forceinline__ bf16x8 without_odd(bf16x8 x) {
   return __builtin_bit_cast(bf16x8, u);
 }
 
-// adds to 4 channels of a row the values of keys from .. end-1 that are not finite
+// adds to 4 channels of a row that has a finite score the values of keys from .. end-1 that are not finite
 __device__ __forceinline__ void add_odd(f32x4& sum, const bf16* v, long stride, int from, int end) {
   for (int n = from; n < end; ++n)
 #pragma unroll

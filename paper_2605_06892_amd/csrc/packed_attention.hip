@@ -248,7 +248,7 @@ __global__ __launch_bounds__(NW * 64) void packed_small_kernel(PackedArgs a, Pac
     const int i = (int)a.by_group.quot(R), hq = h * a.group + R - i * a.group;
     const long orow = (long)(t.q0 + i) * (a.kv_heads * a.group) + hq;
     sum *= l == 0.f ? 0.f : 1.f / l;
-    if (any_odd) add_odd(sum, vg + c, a.v_stride, max(seen_lo, 0) / kKeys * kKeys, keys_seen(a, t, i));
+    if (any_odd && l != 0.f) add_odd(sum, vg + c, a.v_stride, max(seen_lo, 0) / kKeys * kKeys, keys_seen(a, t, i));
     *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.o) + orow * DH + c) = to_bf16x4(sum);
     if (a.lse && c == 0)
       a.lse[orow] = l == 0.f ? -INFINITY : fmaf(m, a.scale, __builtin_amdgcn_logf(l) * kLn2);

@@ -243,7 +243,7 @@ __global__ __launch_bounds__(NW * kWave, DH == 64 ? 4 : 2) void packed_f32_kerne
     sum *= l == 0.f ? 0.f : 1.f / l;
     const int i = (int)a.by_group.quot(R), hq = h * a.group + R - i * a.group;
     const long orow = (long)(t.q0 + i) * (a.kv_heads * a.group) + hq;
-    if (any_odd) {
+    if (any_odd && l != 0.f) {
       const int end = keys_seen(a, t, i);
       for (int n = max(seen_lo, 0) / kKeys * kKeys; n < end; ++n)
 #pragma unroll

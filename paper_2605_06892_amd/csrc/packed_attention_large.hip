@@ -360,7 +360,8 @@ __global__ __launch_bounds__(waves<DH> * 64, 2) void packed_large_kernel(PackedA
 
   // acc[dt][e]: channel dt*32 + (e/4)*8 + hi*4 + e%4 of row l32
   const float l_tot = l_run + __shfl_xor(l_run, 32);
-  const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
+  const bool none = l_tot == 0.f;  // no key, or no finite score: zeros, also where acc holds 0 * infinity
+  const float inv = 1.f / l_tot;
   // The rows go through LDS, so that whole lines of them are stored (8 bytes of
   // a row at a time took 2 us longer).
   __syncthreads();  // every wave is done with the tiles
@@ -373,7 +374,8 @@ __global__ __launch_bounds__(waves<DH> * 64, 2) void packed_large_kernel(PackedA
       const int c = dt * 32 + g * 8 + hi * 4;
       f32x4 v = {acc[dt][4 * g + 0] * inv, acc[dt][4 * g + 1] * inv, acc[dt][4 * g + 2] * inv,
                  acc[dt][4 * g + 3] * inv};
-      if (cut_odd) add_odd(v, vg + c, a.v_stride, n_full * BKV, seen);
+      if (none) v = (f32x4){};
+      else if (cut_odd) add_odd(v, vg + c, a.v_stride, n_full * BKV, seen);
       *reinterpret_cast<bf16x4*>(ol + l32 * DH + (((dt * 4 + g) ^ (l32 & (CPR - 1))) * 8) + hi * 4) = to_bf16x4(v);
     }
   }
@@ -389,7 +391,7 @@ __global__ __launch_bounds__(waves<DH> * 64, 2) void packed_large_kernel(PackedA
     if (rw + r < n_rows) *reinterpret_cast<bf16x8*>(static_cast<bf16*>(a.o) + head_row(rw + r) * DH + c * 8) = x;
   }
   if (a.lse && hi == 0 && rw + l32 < n_rows)
-    a.lse[head_row(rw + l32)] = l_tot == 0.f ? -INFINITY : fmaf(m_ref, a.scale, __builtin_amdgcn_logf(l_tot) * kLn2);
+    a.lse[head_row(rw + l32)] = none ? -INFINITY : fmaf(m_ref, a.scale, __builtin_amdgcn_logf(l_tot) * kLn2);
 }
 
 template <int DH>

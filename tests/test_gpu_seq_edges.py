@@ -1,10 +1,12 @@
-"""GPU tests of the calls over several sequences where memory holds what no row wrote. Definitions, bounds
-and helpers are those of test_gpu_seq.py."""
+"""GPU tests of the calls over several sequences where memory holds what no row wrote, and where no score
+is finite. Definitions, bounds and helpers are those of test_gpu_seq.py."""
+
+import math
 
 import pytest
 import torch
 
-from test_gpu_seq import _gen, check, paged_inputs, paged_want, run_paged
+from test_gpu_seq import _gen, check, form, packed_inputs, packed_want, paged_inputs, paged_want, run_packed, run_paged  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -44,3 +46,47 @@ def test_paged_exponents_of_rows_that_are_not_there(dtype, page, wide, dh, expon
     o, lse = run_paged(q, held, table, lens, page, heads, kv, dh, scale)
     want, lw, A, S = paged_want(q, k, v, table, lens, page, n_pages, heads, kv, dh, scale)
     check(o, lse, want, lw, A, S, dtype, max(lens), dh)
+
+
+def no_finite_scores(k, q, dh, group):
+    """Scores of -infinity for every key and query of the first key/value head: channel 0 is infinite in its keys and
+    negative in its queries."""
+    k[:, 0] = math.inf
+    q[:, :group * dh:dh] = -1.0
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_packed_rows_without_a_finite_score(form, dh, causal):
+    """o = 0 and lse = -infinity where every score is -infinity, whatever the values hold: infinities and NaN in blocks
+    that every row sees whole and in others. The other key/value head is as ever."""
+    dtype, heads, kv, scale = form, 4, 2, dh ** -0.5
+    lens_q, lens_k = [5, 700, 40, 30], [5, 700, 300, 7]
+    q, k, v, cu_q, cu_k = packed_inputs(41, dtype, lens_q, lens_k, heads, kv, dh)
+    no_finite_scores(k, q, dh, heads // kv)
+    for at, x in ((2, math.nan), (5 + 3, math.inf), (5 + 350, -math.inf), (5 + 690, math.nan), (705 + 1, math.inf),
+                  (705 + 299, math.inf), (1005 + 6, -math.inf)):
+        v[at, at % dh] = x
+    o, lse = run_packed(q, k, v, cu_q, cu_k, heads, kv, dh, scale, causal)
+    half = heads // kv
+    assert torch.all(o[:, :half * dh] == 0), o[:, :half * dh].isnan().sum()
+    assert torch.all(lse[:, :half] == -math.inf)
+    want, lw, A, S = packed_want(q[:, half * dh:], k[:, dh:], v[:, dh:], cu_q, cu_k, half, 1, dh, scale, causal)
+    check(o[:, half * dh:], lse[:, half:], want, lw, A, S, dtype, 700, dh)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("page", [24, 64])
+@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("dh", [64, 128])
+def test_paged_rows_without_a_finite_score(dtype, page, wide, dh):
+    heads, kv, lens, scale = 4, 2, [700, 33, 1], dh ** -0.5
+    q, k, v, held, table = paged_inputs(42, dtype, dtype, lens, page, heads, kv, dh, max_pages=5000 // page if wide else None)
+    no_finite_scores(k, q, dh, heads // kv)
+    v[::7, 3], v[::11, 5], v[::13, 9] = math.inf, -math.inf, math.nan
+    o, lse = run_paged(q, (k, v, None, None), table, lens, page, heads, kv, dh, scale)
+    half = heads // kv
+    assert torch.all(o[:, :half * dh] == 0), o[:, :half * dh].isnan().sum()
+    assert torch.all(lse[:, :half] == -math.inf)
+    want, lw, A, S = paged_want(q[:, half * dh:], k[:, dh:], v[:, dh:], table, lens, page, k.shape[0] // page, half, 1, dh, scale)
+    check(o[:, half * dh:], lse[:, half:], want, lw, A, S, dtype, 700, dh)
