@@ -296,6 +296,8 @@ struct Attend {
       f32x4 sc[KT] = {};
       float vf[F32 ? 4 : 1][DT];
       if constexpr (F32) {
+        // codes times their exponent before the products, which could overflow without it
+        const float sk = E4M3 ? pow2(ke[0]) : 1.f;
 #pragma unroll
         for (int i = 0; i < KL; ++i)
 #pragma unroll
@@ -304,7 +306,7 @@ struct Attend {
             if constexpr (E4M3) {
               const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)kr[0][i][j], false);
               const f32x2 up = __builtin_amdgcn_cvt_pk_f32_fp8((int)kr[0][i][j], true);
-              x[0] = lo[0], x[1] = lo[1], x[2] = up[0], x[3] = up[1];
+              x[0] = lo[0] * sk, x[1] = lo[1] * sk, x[2] = up[0] * sk, x[3] = up[1] * sk;
             } else {
               x[0] = __uint_as_float(kr[0][i][j]);
             }
@@ -330,10 +332,6 @@ struct Attend {
           if (cut && !(keys >> v_key(i) & 1))
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) vf[i][dt] = 0.f;
-        }
-        if constexpr (E4M3) {  // the keys' exponents, from the lanes that loaded them
-#pragma unroll
-          for (int e = 0; e < 4; ++e) sc[0][e] *= pow2(__shfl(ke[0], grp * 4 + e));
         }
       } else {
 #pragma unroll

@@ -1,5 +1,5 @@
-"""GPU tests of the calls over several sequences where memory holds what no row wrote, and where no score
-is finite. Definitions, bounds and helpers are those of test_gpu_seq.py."""
+"""GPU tests of the calls over several sequences where memory holds what no row wrote, where no score is
+finite, and at the limits of fp32. Definitions, bounds and helpers are those of test_gpu_seq.py."""
 
 import math
 
@@ -90,3 +90,22 @@ def test_paged_rows_without_a_finite_score(dtype, page, wide, dh):
     assert torch.all(lse[:, :half] == -math.inf)
     want, lw, A, S = paged_want(q[:, half * dh:], k[:, dh:], v[:, dh:], table, lens, page, k.shape[0] // page, half, 1, dh, scale)
     check(o[:, half * dh:], lse[:, half:], want, lw, A, S, dtype, 700, dh)
+
+
+@pytest.mark.parametrize("page", [24, 64])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("small", ["keys", "queries"])
+def test_paged_f32_queries_and_codes_of_very_different_magnitude(dh, page, small):
+    """Queries around 2^120 over keys around 2^-110: their products fit fp32, those of queries and codes, without the
+    exponents, do not. And 2^-112 over 2^112."""
+    heads, kv, lens = 4, 2, [90, 33]
+    q, k, v, held, table = paged_inputs(43, "f32", "e4m3", lens, page, heads, kv, dh)
+    up, down = (120, -110) if small == "keys" else (-112, 112)
+    q = q.clamp(-3, 3) * 2.0 ** up
+    held[2].copy_((held[2].long() + down).clamp(-117, 119).to(torch.int8))
+    codes = held[0].float().double().view(-1, kv, dh)
+    k = (codes * torch.pow(2.0, held[2].double())[..., None]).view(k.shape)
+    scale = 2.0 ** -(up + down) * dh ** -0.5
+    o, lse = run_paged(q, held, table, lens, page, heads, kv, dh, scale)
+    want, lw, A, S = paged_want(q, k, v, table, lens, page, k.shape[0] // page, heads, kv, dh, scale)
+    check(o, lse, want, lw, A, S, "f32", 90, dh)
