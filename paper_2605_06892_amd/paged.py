@@ -56,9 +56,12 @@ class PagedCache:
 
 
 def slots(page_table: np.ndarray, page_size: int, seqs, positions) -> np.ndarray:
-    """Cache rows (int32) of the tokens at `positions` of sequences `seqs`, by the host's table of pages."""
+    """Cache rows (int32) of the tokens at `positions` of sequences `seqs`, by the host's table of pages. -1 (no row)
+    for a negative sequence, position or page number, and for a page whose rows do not fit int32."""
     seqs, positions = np.asarray(seqs), np.asarray(positions)
-    return (page_table[seqs, positions // page_size].astype(np.int64) * page_size + positions % page_size).astype(np.int32)
+    pages = page_table[np.maximum(seqs, 0), np.maximum(positions, 0) // page_size].astype(np.int64)
+    rows = pages * page_size + positions % page_size
+    return np.where((seqs < 0) | (positions < 0) | (pages < 0) | (rows > 2 ** 31 - 1), -1, rows).astype(np.int32)
 
 
 def prefill(c: PagedCache, q, k, v, cu, idx, heads: int, o, lse=None) -> None:
