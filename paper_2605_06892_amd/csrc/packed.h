@@ -11,8 +11,6 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdio>
-#include <cstdlib>
 
 namespace hsa {
 
@@ -160,15 +158,22 @@ struct PackedCost {
   int rows, waves;
   double fixed, tile, block, chain;
 };
-// The cheapest of N shapes; HSA_PACKED_TILE=<rows>x<waves> forces one for measurement
-// sweeps and tests.
+// The tile forced for this thread's launches (packed_tile.h); rows 0: none. 128 and 256 rows both
+// mean the large kernel, which has one of them for either width.
+struct PackedTile {
+  int rows, waves;
+  bool is(const PackedCost& c) const { return rows == c.rows && waves == c.waves; }
+  bool large() const { return (rows == 128 && waves == 4) || (rows == 256 && waves == 8); }
+};
+PackedTile& packed_tile();
+// The cheapest of N shapes; NULL where one is forced that is none of them.
 template <int N>
-inline PackedCost packed_choice(const PackedArgs& a, const PackedCost (&costs)[N]) {
-  if (const char* forced = getenv("HSA_PACKED_TILE")) {
-    int rows = 0, waves = 0;
-    if (sscanf(forced, "%dx%d", &rows, &waves) == 2)
-      for (const PackedCost& c : costs)
-        if (c.rows == rows && c.waves == waves) return c;
+inline const PackedCost* packed_choice(const PackedArgs& a, const PackedCost (&costs)[N]) {
+  const PackedTile forced = packed_tile();
+  if (forced.rows) {
+    for (const PackedCost& c : costs)
+      if (forced.is(c) || (forced.large() && c.rows >= 128)) return &c;
+    return nullptr;
   }
   const double seqs = a.n_seqs, len_q = a.n_q / seqs, len_k = a.n_kv / seqs;
   const double blocks = std::max(0.0, len_k - (a.causal ? len_q / 2 : 0.0)) / 32;
@@ -184,7 +189,7 @@ inline PackedCost packed_choice(const PackedArgs& a, const PackedCost (&costs)[N
       least = us;
     }
   }
-  return *best;
+  return best;
 }
 
 hipError_t launch_packed_attention_f32(const PackedArgs& a, int head_dim, hipStream_t s);

@@ -15,10 +15,7 @@
 // subtraction of the running maximum in fp32. Rounded to bf16 are the probabilities
 // (the sum takes them before that) and the output.
 #include "packed.h"
-
-#include <algorithm>
-#include <cmath>
-#include <cstdlib>
+#include "packed_tile.h"
 
 namespace hsa {
 namespace {
@@ -287,13 +284,19 @@ constexpr PackedCost kCosts[2][5] = {{{16, 8, 2.5, 2.0, 0.132, 0.060},   // 64-w
 
 template <int DH>
 hipError_t launch_dh(const PackedArgs& a, hipStream_t s) {
-  const PackedCost c = packed_choice(a, kCosts[DH == 128]);
-  if (c.rows >= 128) return launch_packed_attention_large(a, DH, s);
-  if (c.rows == 32) return c.waves == 8 ? launch_small<DH, 32, 8>(a, s) : launch_small<DH, 32, 4>(a, s);
-  return c.waves == 8 ? launch_small<DH, 16, 8>(a, s) : launch_small<DH, 16, 4>(a, s);
+  const PackedCost* c = packed_choice(a, kCosts[DH == 128]);
+  if (!c) return hipErrorInvalidValue;
+  if (c->rows >= 128) return launch_packed_attention_large(a, DH, s);
+  if (c->rows == 32) return c->waves == 8 ? launch_small<DH, 32, 8>(a, s) : launch_small<DH, 32, 4>(a, s);
+  return c->waves == 8 ? launch_small<DH, 16, 8>(a, s) : launch_small<DH, 16, 4>(a, s);
 }
 
 }  // namespace
+
+PackedTile& packed_tile() {
+  static thread_local PackedTile tile{0, 0};
+  return tile;
+}
 
 hipError_t launch_packed_attention(const PackedArgs& a, bool bf16, int head_dim, hipStream_t s) {
   if (a.n_q <= 0 || a.n_seqs <= 0) return hipSuccess;
@@ -302,3 +305,5 @@ hipError_t launch_packed_attention(const PackedArgs& a, bool bf16, int head_dim,
 }
 
 }  // namespace hsa
+
+void _hsa_packed_tile(int rows, int waves) { hsa::packed_tile() = {rows, waves}; }

@@ -275,8 +275,9 @@ constexpr PackedCost kCosts[2][2] = {{{W, 8, 3.6, 3.2, 0.329, 0.062}, {W, 4, 5.6
 
 template <int DH>
 hipError_t launch_dh(const PackedArgs& a, hipStream_t s) {
-  const PackedCost c = packed_choice(a, kCosts[DH == 128]);
-  return c.waves == 4 ? launch_waves<DH, 4>(a, s) : launch_waves<DH, 8>(a, s);
+  const PackedCost* c = packed_choice(a, kCosts[DH == 128]);
+  if (!c) return hipErrorInvalidValue;
+  return c->waves == 4 ? launch_waves<DH, 4>(a, s) : launch_waves<DH, 8>(a, s);
 }
 
 }  // namespace

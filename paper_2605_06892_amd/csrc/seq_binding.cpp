@@ -9,10 +9,13 @@
 
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cstdio>
+#include <cstdlib>
 #include <exception>
 #include <string>
 
 #include "../../include/hsa_step.h"
+#include "packed_tile.h"
 
 namespace {
 
@@ -173,6 +176,22 @@ int cache(Args& a, bool store) {
                         kv_heads, head_dim, dt, k.data_ptr(), row_stride(k), v.data_ptr(), row_stride(v), stream);
 }
 
+// The tile that HSA_PACKED_TILE asks for, this thread's launches' until it goes.
+struct Forced {
+  int rows = 0, waves = 0;
+  Forced() {  // with the interpreter held
+    const char* tile = getenv("HSA_PACKED_TILE");
+    if (!tile || !*tile) return;
+    char rest;
+    if (sscanf(tile, "%dx%d%c", &rows, &waves, &rest) != 2 || rows < 1 || waves < 1)
+      value_error("HSA_PACKED_TILE is <rows>x<waves>, got " + std::string(tile));
+    _hsa_packed_tile(rows, waves);
+  }
+  ~Forced() {
+    if (rows) _hsa_packed_tile(0, 0);
+  }
+};
+
 // (device, stream, q, k, v, cu_q, cu_kv, heads, kv_heads, head_dim, scale, causal, o, lse)
 int packed(Args& a) {
   const Here here{a.integer()};
@@ -199,6 +218,7 @@ int packed(Args& a) {
       q.size(1) != (int64_t)heads * head_dim || o.sizes() != q.sizes() || k.size(1) != (int64_t)kv_heads * head_dim ||
       v.sizes() != k.sizes())
     value_error("q and o are [n_q, heads * head_dim], k and v [n_kv, kv_heads * head_dim], cu_q and cu_kv [n_seqs + 1]");
+  const Forced forced;
   const Unlocked unlocked;
   return hsa_packed_attention(dt, q.data_ptr(), row_stride(q), k.data_ptr(), row_stride(k), v.data_ptr(), row_stride(v),
                               ints(cu_q), ints(cu_kv), (int32_t)(cu_q.numel() - 1), q.size(0), k.size(0), heads, kv_heads,

@@ -6,6 +6,7 @@ import math
 import pytest
 import torch
 
+from paper_2605_06892_amd import hsa_step as H
 from test_gpu_seq import _gen, check, form, packed_inputs, packed_want, paged_inputs, paged_want, run_packed, run_paged  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -109,3 +110,24 @@ def test_paged_f32_queries_and_codes_of_very_different_magnitude(dh, page, small
     o, lse = run_paged(q, held, table, lens, page, heads, kv, dh, scale)
     want, lw, A, S = paged_want(q, k, v, table, lens, page, k.shape[0] // page, heads, kv, dh, scale)
     check(o, lse, want, lw, A, S, "f32", 90, dh)
+
+
+def test_packed_forced_tiles(monkeypatch):
+    """HSA_PACKED_TILE: 128 and 256 rows both mean the large kernel, whichever it has for the width; a shape that no
+    kernel has is refused; the variable is read at every call."""
+    q, k, v, cu, _ = packed_inputs(44, "bf16", [300], [300], 2, 1, 128)
+    outs = {}
+    for tile in ("16x4", "16x8", "32x4", "128x4", "256x8"):
+        monkeypatch.setenv("HSA_PACKED_TILE", tile)
+        outs[tile] = run_packed(q, k, v, cu, cu, 2, 1, 128, 0.1, True)[1]
+    assert torch.equal(outs["128x4"], outs["256x8"])
+    assert not torch.equal(outs["16x4"], outs["256x8"]) and not torch.equal(outs["16x8"], outs["16x4"])
+    for tile in ("17x4", "16x5", "128x8", "0x0", "-16x4", "16", "large", "32x4 "):
+        monkeypatch.setenv("HSA_PACKED_TILE", tile)
+        with pytest.raises(H.HsaStepError if tile in ("17x4", "16x5", "128x8") else ValueError):
+            run_packed(q, k, v, cu, cu, 2, 1, 128, 0.1, True)
+    monkeypatch.setenv("HSA_PACKED_TILE", "32x4")
+    with pytest.raises(H.HsaStepError):  # fp32 has no 32-row tile
+        run_packed(q.float(), k.float(), v.float(), cu, cu, 2, 1, 128, 0.1, True)
+    monkeypatch.delenv("HSA_PACKED_TILE")
+    run_packed(q, k, v, cu, cu, 2, 1, 128, 0.1, True)
