@@ -29,16 +29,16 @@ __device__ __forceinline__ int xcd_contiguous(int L, int total) {
   return xcd * base + (xcd < rem ? xcd : rem) + slot;
 }
 
-// Compute units of the current device (queried once; 256 if the query fails).
+// Compute units of the current device (queried once, also by threads that launch at the same
+// time; 256 if the query fails).
 inline int compute_units() {
-  static int cus = 0;
-  if (!cus) {
+  static const int cus = [] {
     int dev = 0, n = 0;
-    cus = (hipGetDevice(&dev) == hipSuccess &&
-           hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0)
-              ? n
-              : 256;
-  }
+    return hipGetDevice(&dev) == hipSuccess &&
+                   hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0
+               ? n
+               : 256;
+  }();
   return cus;
 }
 
