@@ -2,9 +2,9 @@
 
 Every translation unit under csrc/ is compiled to an object in parallel with
 hipcc, then linked into a shared library next to this file. Only the C ABI
-symbols are exported (hidden visibility, -Bsymbolic binding). _seq_binding.so, the
-Python binding of the calls over several sequences, is host code against torch's
-headers and that library.
+symbols are exported (hidden visibility, -Bsymbolic binding), and one of the binding's
+(csrc/packed_tile.h). _seq_binding.so, the Python binding of the calls over several
+sequences, is host code against torch's headers and that library.
 
     python -m paper_2605_06892_amd.build
 """
@@ -85,7 +85,9 @@ def _link_binding(obj: str) -> None:
 
 
 def build(jobs: int | None = None) -> str:
-    """Compile and link the library; returns its path. Always rebuilds."""
+    """Compile and link the library and its binding; returns the library's path. Always
+    rebuilds. What only the binding needs (g++, torch's headers) does not keep the library from
+    being built: without it the library is in place when this raises, and a former binding is not."""
     os.makedirs(OBJ, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
     if not srcs:
@@ -94,14 +96,18 @@ def build(jobs: int | None = None) -> str:
     with ThreadPoolExecutor(jobs) as ex:
         binding = ex.submit(_compile_binding)
         objs = list(ex.map(_compile, srcs))
-        binding_obj = binding.result()
     tmp = LIB + ".tmp"
     cmd = [hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", "-Wl,-Bsymbolic", "-o", tmp, *objs]
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}")
     os.replace(tmp, LIB)
-    _link_binding(binding_obj)
+    try:
+        _link_binding(binding.result())
+    except Exception as e:
+        if os.path.exists(BINDING):
+            os.remove(BINDING)
+        raise RuntimeError(f"{LIB} is built, its binding of the calls over several sequences is not: {e}") from e
     return LIB
 
 

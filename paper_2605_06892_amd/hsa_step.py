@@ -439,7 +439,11 @@ def _binding():
     global _seq
     if _seq is None:
         lib()  # says what to do if nothing was built
-        from . import _seq_binding
+        try:
+            from . import _seq_binding
+        except ImportError as e:
+            raise ImportError(f"the binding of the calls over several sequences was not built ({e}): build it with "
+                              "`python -m paper_2605_06892_amd.build`") from e
         _seq = _seq_binding
     return _seq
 
