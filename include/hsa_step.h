@@ -621,7 +621,7 @@ int hsa_cache_load(int cache_dtype, const void* k_cache, const void* v_cache, co
  *               as they were.
  *   o           [n_q, heads * head_dim] dtype, contiguous
  *   lse         NULL or [n_q, heads] fp32
- *   scale       > 0, finite
+ *   scale       > 0, at most 2^127
  * n_q * heads / 16 + (n_seqs + 8) * kv_heads < 2^23, n_kv <= 2^30. o and lse must not overlap an input or
  * each other.
  */
@@ -658,6 +658,7 @@ size_t hsa_paged_attention_workspace_bytes(int dtype, int32_t n_seqs, int32_t he
  *   k_cache, ... as for hsa_cache_store, with n_pages * page_size rows
  *   page_table   int32 [n_seqs, max_pages]; pages may be shared by sequences
  *   kv_lens      int32 [n_seqs] on the device, clamped to [0, max_pages * page_size]
+ *   scale        > 0, at most 2^127
  *   o            [n_seqs, heads * head_dim] dtype, contiguous
  *   lse          NULL or [n_seqs, heads] fp32
  *   workspace    device scratch of hsa_paged_attention_workspace_bytes(dtype,

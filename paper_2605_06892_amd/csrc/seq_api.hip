@@ -1,7 +1,5 @@
 // C ABI entry points of the calls over several sequences: host-side argument
 // checks, then kernel launches. See include/hsa_step.h for their contract.
-#include <math.h>
-
 #include "api_util.h"
 #include "seq_common.h"
 
@@ -28,6 +26,9 @@ bool heads_ok(int32_t heads, int32_t kv_heads, int32_t head_dim) {
   return heads > 0 && kv_heads > 0 && heads % kv_heads == 0 && (head_dim == 64 || head_dim == 128) &&
          (int64_t)heads * head_dim <= kMaxStride;
 }
+
+// the kernels take scale * log2(e) in fp32
+bool scale_ok(float scale) { return scale > 0.f && scale <= 0x1p127f; }
 
 struct Range {
   const void* p;
@@ -151,7 +152,7 @@ HSA_API int hsa_packed_attention(int dtype, const void* q, int64_t q_stride, con
   const size_t es = elem_size(dtype);
   if (!es) return HSA_STEP_ERR_DTYPE;
   if (!heads_ok(heads, kv_heads, head_dim) || n_seqs < 0 || n_seqs == INT32_MAX || n_q < 0 || n_kv < 0 ||
-      n_q > kMaxRows / heads || n_kv > kMaxKeys || !(scale > 0.f) || !isfinite(scale))
+      n_q > kMaxRows / heads || n_kv > kMaxKeys || !scale_ok(scale))
     return HSA_STEP_ERR_SHAPE;
   // one launch: fewer than 2^32 threads, 512 per 16 rows or item
   if (n_q * heads / 16 + ((int64_t)n_seqs + 8) * kv_heads >= kMaxLaunch / 512) return HSA_STEP_ERR_SHAPE;
@@ -207,7 +208,7 @@ HSA_API int hsa_paged_attention(int dtype, const void* q, int64_t q_stride, int 
   if (!es || !ce) return HSA_STEP_ERR_DTYPE;
   if (!heads_ok(heads, kv_heads, head_dim) || n_seqs < 0 || n_seqs > kMaxRows / heads || n_pages < 0 ||
       max_pages < 0 || page_size < 1 || (int64_t)n_pages * page_size > kMaxRows ||
-      (int64_t)max_pages * page_size > kMaxKeys || !(scale > 0.f) || !isfinite(scale))
+      (int64_t)max_pages * page_size > kMaxKeys || !scale_ok(scale))
     return HSA_STEP_ERR_SHAPE;
   const int64_t d = (int64_t)heads * head_dim, dk = (int64_t)kv_heads * head_dim;
   const int64_t n_rows = (int64_t)n_pages * page_size;

@@ -150,3 +150,11 @@ def test_binding_refuses_host_tensors():
         H.hsa_packed_attention(x, x, x, i, i, 2, 2, 128, 0.1, True, x)
     with pytest.raises(ValueError):
         H.hsa_paged_attention(x, x, x, i.view(4, 1), i, 16, 2, 2, 128, 0.1, x, None)
+
+
+@pytest.mark.parametrize("scale,status", [(2.0 ** 127, OK), (2.0 ** 127 * (1 + 2.0 ** -23), SHAPE), (3.4028234e38, SHAPE)])
+def test_scales_whose_product_with_log2_e_is_infinite(lib, scale, status):
+    """The bf16 forms take scale * log2(e) in fp32: refused where that is not finite, and up to 2^127 it is."""
+    # with nothing to do, so that the scale is all that is checked
+    assert _call(lib.hsa_packed_attention, PACKED, n_seqs=0, scale=scale) == status
+    assert _call(lib.hsa_paged_attention, PAGED, n_seqs=0, scale=scale) == status
