@@ -29,7 +29,7 @@ class PagedCache:
     v: torch.Tensor
     k_exp: torch.Tensor | None  # int8 [n_pages * page_size, kv_heads] with codes
     v_exp: torch.Tensor | None
-    workspace: torch.Tensor    # uint8, the decoding step's
+    workspace: torch.Tensor    # uint8, the decoding step's; steps that may overlap in time need one each
     page_size: int
     kv_heads: int
     head_dim: int
@@ -44,14 +44,15 @@ class PagedCache:
 
     @classmethod
     def allocate(cls, n_pages: int, page_size: int, kv_heads: int, head_dim: int, dtype: torch.dtype,
-                 device="cuda", e4m3: bool = False) -> "PagedCache":
-        """e4m3 keeps the rows in 8 bits (one exponent per row and head), half of bf16's bytes."""
+                 device="cuda", e4m3: bool = False, workspace: torch.Tensor | None = None) -> "PagedCache":
+        """e4m3 keeps the rows in 8 bits (one exponent per row and head), half of bf16's bytes. workspace: another
+        layer's cache's, for layers whose steps follow each other in one stream; None allocates one."""
         rows, d = n_pages * page_size, kv_heads * head_dim
         e = lambda *s, dt=dtype: torch.empty(*s, dtype=dt, device=device)  # noqa: E731
         held = torch.float8_e4m3fn if e4m3 else dtype
         exps = [e(rows, kv_heads, dt=torch.int8) if e4m3 else None for _ in range(2)]
         return cls(k=e(rows, d, dt=held), v=e(rows, d, dt=held), k_exp=exps[0], v_exp=exps[1],
-                   workspace=e(H.PAGED_WORKSPACE_BYTES, dt=torch.uint8), page_size=page_size, kv_heads=kv_heads,
+                   workspace=e(H.PAGED_WORKSPACE_BYTES, dt=torch.uint8) if workspace is None else workspace, page_size=page_size, kv_heads=kv_heads,
                    head_dim=head_dim)
 
 

@@ -33,3 +33,13 @@ def test_page_numbers_past_the_int32_rows():
 def test_positions_past_the_table():
     with pytest.raises(IndexError):
         paged.slots(TABLE, 16, [0], [48])
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_layers_may_share_one_workspace(e4m3):
+    import torch
+
+    a = paged.PagedCache.allocate(4, 16, 2, 64, torch.float32, device="cpu", e4m3=e4m3)
+    b = paged.PagedCache.allocate(4, 16, 2, 64, torch.float32, device="cpu", e4m3=e4m3, workspace=a.workspace)
+    assert b.workspace is a.workspace and a.workspace.numel() == paged.H.PAGED_WORKSPACE_BYTES
+    assert b.k.data_ptr() != a.k.data_ptr() and b.n_pages == 4
