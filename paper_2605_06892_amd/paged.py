@@ -51,9 +51,10 @@ class PagedCache:
         e = lambda *s, dt=dtype: torch.empty(*s, dtype=dt, device=device)  # noqa: E731
         held = torch.float8_e4m3fn if e4m3 else dtype
         exps = [e(rows, kv_heads, dt=torch.int8) if e4m3 else None for _ in range(2)]
-        return cls(k=e(rows, d, dt=held), v=e(rows, d, dt=held), k_exp=exps[0], v_exp=exps[1],
-                   workspace=e(H.PAGED_WORKSPACE_BYTES, dt=torch.uint8) if workspace is None else workspace, page_size=page_size, kv_heads=kv_heads,
-                   head_dim=head_dim)
+        if workspace is None:
+            workspace = e(H.PAGED_WORKSPACE_BYTES, dt=torch.uint8)
+        return cls(k=e(rows, d, dt=held), v=e(rows, d, dt=held), k_exp=exps[0], v_exp=exps[1], workspace=workspace,
+                   page_size=page_size, kv_heads=kv_heads, head_dim=head_dim)
 
 
 def slots(page_table: np.ndarray, page_size: int, seqs, positions) -> np.ndarray:
