@@ -561,6 +561,12 @@ int hsa_stack_iteration(const hsa_stack* stack, int32_t T, int32_t iter, int32_t
  * is within half a step of the code, 2^-4 of itself, or within 2^(e-10) where
  * that is more, and is exact in bf16.
  *
+ * The attention calls compute scores, softmax statistics and weighted sums in fp32.
+ * With bf16 rows the softmax weights are rounded to bf16 before they multiply the
+ * values (half a step, 2^-8 of each; the sum of the weights takes them before
+ * that), and the output is rounded to bf16. With fp32 rows, e4m3 caches among
+ * them, nothing is rounded to fewer bits.
+ *
  * Row indices and page numbers outside the cache are skipped, never followed.
  * head_dim is 64 or 128, heads * head_dim at most 2^22. Row strides are in
  * elements, at least the row's width and at most 2^22; rows of bf16 inputs are
@@ -623,7 +629,9 @@ int hsa_cache_load(int cache_dtype, const void* k_cache, const void* v_cache, co
  *   lse         NULL or [n_q, heads] fp32
  *   scale       > 0, at most 2^127
  * n_q * heads / 16 + (n_seqs + 8) * kv_heads < 2^23, n_kv <= 2^30. o and lse must not overlap an input or
- * each other.
+ * each other. The host knows the mean lengths only and chooses the kernel by them:
+ * one long sequence among hundreds of single tokens may take more than three times
+ * as long as alone. Two calls, the long ones and the short ones, do not.
  */
 int hsa_packed_attention(int dtype, const void* q, int64_t q_stride, const void* k,
                          int64_t k_stride, const void* v, int64_t v_stride, const int32_t* cu_q,
