@@ -155,7 +155,7 @@ def _quantize(x):
     step = torch.where(mag < 2, 0.5, torch.where(mag < 4, 1.0, 2.0))
     mag = torch.round(mag / step) * step
     code = torch.where(mag < 2, 2 * mag, torch.where(mag < 4, mag + 2, mag / 2 + 4)).to(torch.uint8)
-    code = (code + 8 * torch.signbit(y)).view(*x.shape)
+    code = (code + 8 * torch.signbit(y).to(torch.uint8)).view(*x.shape)
     return code[..., 0::2] + 16 * code[..., 1::2], ex.to(torch.int8)
 
 
