@@ -69,7 +69,8 @@ typedef enum hsa_step_status {
 typedef enum hsa_step_dtype {
   HSA_STEP_F32 = 0,
   HSA_STEP_BF16 = 1,
-  HSA_STEP_E4M3 = 2 /* 8-bit cache rows, only where an entry point has a cache_dtype */
+  HSA_STEP_E4M3 = 2, /* 8-bit cache rows, only where an entry point has a cache_dtype */
+  HSA_STEP_E2M1 = 4  /* 4-bit cache rows, the same */
 } hsa_step_dtype;
 
 /* How a multi-layer loop sets group membership (Appendix B). */
@@ -540,7 +541,8 @@ int hsa_stack_iteration(const hsa_stack* stack, int32_t T, int32_t iter, int32_t
                         hipStream_t stream);
 
 /* ------------------------------------------------------------------------
- * Sequences: caches in 8 bits or in pages, attention of several sequences.
+ * Sequences: caches in 8 or 4 bits or in pages, attention of several sequences, and
+ * the calls of a decoding step around it.
  *
  * The calls above serve one sample whose queries see every cached row. These
  * serve many sequences at once: a batch of samples with active sets of
@@ -561,10 +563,19 @@ int hsa_stack_iteration(const hsa_stack* stack, int32_t T, int32_t iter, int32_t
  * is within half a step of the code, 2^-4 of itself, or within 2^(e-10) where
  * that is more, and is exact in bf16.
  *
+ * HSA_STEP_E2M1 holds rows in 4 bits: every 32 consecutive values (a group) are 16 bytes
+ * of codes, the value of even index in the low half of its byte, and one signed exponent e; code
+ * c stands for (-1)^(c >> 3) * {0, 0.5, 1, 1.5, 2, 3, 4, 6}[c & 7] * 2^e. e is the smallest
+ * integer in [-125, 125] with max |x| <= 6 * 2^e over the group, and the codes are x * 2^-e
+ * rounded to nearest, ties to the even code, saturating. A group that holds a value which is not
+ * finite has e = -128 and reads as 32 NaN. A value read back is within a quarter of
+ * itself, or within 2^(e-2) where that is more, and is exact in bf16. Exponents
+ * other than those are not made here, and what they stand for is unspecified.
+ *
  * The attention calls compute scores, softmax statistics and weighted sums in fp32.
  * With bf16 rows the softmax weights are rounded to bf16 before they multiply the
  * values (half a step, 2^-8 of each; the sum of the weights takes them before
- * that), and the output is rounded to bf16. With fp32 rows, e4m3 caches among
+ * that), and the output is rounded to bf16. With fp32 rows, caches of codes among
  * them, nothing is rounded to fewer bits.
  *
  * Row indices and page numbers outside the cache are skipped, never followed.
@@ -575,7 +586,7 @@ int hsa_stack_iteration(const hsa_stack* stack, int32_t T, int32_t iter, int32_t
 
 /*
  * Fresh keys and values into cache rows, quantized as they are written for
- * HSA_STEP_E4M3. For j < n with t = idx[j]:
+ * HSA_STEP_E4M3 and HSA_STEP_E2M1. For j < n with t = idx[j]:
  *   k_cache[t] = k[j], v_cache[t] = v[j]
  * Rows not in idx are not written; an index outside [0, n_rows) (-1 for a
  * padded position) skips its row. n * kv_heads * head_dim < 2^34.
@@ -583,8 +594,9 @@ int hsa_stack_iteration(const hsa_stack* stack, int32_t T, int32_t iter, int32_t
  *                    v_stride elements apart (slices of one projection's output)
  *   idx              int32 [n], duplicate-free apart from skipped entries
  *   k_cache, v_cache [n_rows, kv_heads * head_dim] cache_dtype, 16-byte aligned
- *                    (fp32: 4)
- *   k_exp, v_exp     int8 [n_rows, kv_heads], HSA_STEP_E4M3 only (else ignored)
+ *                    (fp32: 4); HSA_STEP_E2M1: bytes [n_rows, kv_heads * head_dim / 2]
+ *   k_exp, v_exp     int8 [n_rows, kv_heads] for HSA_STEP_E4M3, [n_rows, kv_heads *
+ *                    head_dim / 32] for HSA_STEP_E2M1 (else ignored)
  * The caches must not overlap the inputs, idx, the exponents or each other.
  */
 int hsa_cache_store(int dtype, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
@@ -594,8 +606,8 @@ int hsa_cache_store(int dtype, const void* k, int64_t k_stride, const void* v, i
 
 /*
  * Cache rows read back: k[j] = k_cache[idx[j]], v[j] = v_cache[idx[j]] for
- * j < n, in dtype (exact: the codes' values for HSA_STEP_E4M3, a copy
- * otherwise). An index may come twice; one outside [0, n_rows) gives a row of
+ * j < n, in dtype (exact: the codes' values for HSA_STEP_E4M3 and HSA_STEP_E2M1, a
+ * copy otherwise). An index may come twice; one outside [0, n_rows) gives a row of
  * zeros. Arguments as for hsa_cache_store; k and v must not overlap the caches,
  * the exponents, idx or each other, each taken from its first row to the end
  * of its last (what lies between the rows is left as it was).
@@ -683,6 +695,92 @@ int hsa_paged_attention(int dtype, const void* q, int64_t q_stride, int cache_dt
                         int32_t page_size, int32_t heads, int32_t kv_heads, int32_t head_dim,
                         float scale, void* o, float* lse, void* workspace, size_t workspace_bytes,
                         hipStream_t stream);
+
+/*
+ * Weights into 4 bits: rows of HSA_STEP_E2M1 groups as above, along the rows of w.
+ *   w      [n_rows, d] dtype, rows w_stride elements apart (16-byte aligned rows for bf16)
+ *   codes  bytes [n_rows, d / 2], 16-byte aligned     exps  int8 [n_rows, d / 32]
+ * d a multiple of 32, at most 2^22; n_rows * d < 2^35 - 2048. codes and exps must not overlap w or
+ * each other.
+ */
+int hsa_quantize_w4(int dtype, const void* w, int64_t w_stride, int64_t n_rows, int32_t d,
+                    void* codes, int8_t* exps, hipStream_t stream);
+
+/*
+ * hsa_linear with weights in 4 bits, for a few rows (a decoding step's tokens):
+ *   y[m] = act(s[m] (x[m] W^T)) (+ residual[m]),  m < n_rows,
+ * W[o][i] the value of the i-th code of row o of w. The products are exact, sums are in fp32
+ * and rounded once to out_dtype. Its time is that of reading the weights up to some 64 rows and
+ * in proportion to the rows beyond; a prompt's rows are better served by hsa_linear.
+ *   x          [n_rows, d_in] dtype
+ *   w, w_exp   [d_out, d_in / 2] bytes and [d_out, d_in / 32] int8, from hsa_quantize_w4
+ *   row_scale  NULL or [n_rows] fp32
+ *   residual   NULL or [n_rows, d_out] out_dtype; it may be y itself, but must not overlap
+ *              y otherwise
+ *   y          [n_rows, d_out] out_dtype
+ * out_dtype is dtype, or HSA_STEP_F32 with dtype HSA_STEP_BF16 (then no residual and no
+ * GELU); GELU takes no residual. d_in is a multiple of 32; d_in, d_out and n_rows are at most
+ * 2^22; x, w, residual and y are 16-byte aligned. y must not overlap x, w, w_exp or row_scale.
+ */
+int hsa_linear_w4(int dtype, const void* x, int32_t n_rows, int32_t d_in, const void* w,
+                  const int8_t* w_exp, int32_t d_out, const float* row_scale, const void* residual,
+                  int32_t gelu, int out_dtype, void* y, hipStream_t stream);
+
+/*
+ * RMS norms of every head of queries and keys and their rotation by position, rounded
+ * once: for row j and head h, with x the head's head_dim channels,
+ *   z = x / sqrt(mean over c of x_c^2 + eps) * weight
+ * and the first rope_dim channels of z turned in pairs by row pos[j] of the table,
+ *   (a, b) -> (a cos - b sin, a sin + b cos),
+ * pair i being the channels (2i, 2i + 1) with interleaved != 0 and (i, i + rope_dim / 2)
+ * otherwise. Computed in fp32 (the sum of squares in 64 bits where fp32 cannot hold it). A
+ * position outside [0, n_pos) (-1 for a padded token) leaves its row normed and not turned.
+ *   q, q_out  [n, heads * head_dim] dtype, rows q_stride and q_out_stride elements apart
+ *   k, k_out  [n, kv_heads * head_dim], the same. heads or kv_heads may be 0
+ *   q_weight, k_weight  NULL (ones) or [head_dim] dtype, for every head the same
+ *   eps       > 0, at most 2^127
+ *   rope      fp32 (cos, sin) pairs [n_pos, rope_dim / 2], 16-byte aligned; not read if
+ *             rope_dim is 0. One row per position, or per token of a grid (then the sum of the
+ *             rows of hsa_rope_table that its coordinates have)
+ *   rope_dim  0 (no rotation) to head_dim, a multiple of 8
+ *   pos       int32 [n], or NULL: row j is at position j
+ * q_out may be q and k_out k, each with its own stride. Otherwise no output row may overlap another row;
+ * rows that lie between each other's, with equal strides, are separate. Weights and
+ * q, k, q_out, k_out of bf16 are 16-byte aligned. n * (heads + kv_heads) * head_dim < 2^35 - 2048.
+ */
+int hsa_qk_norm_rope(int dtype, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                     int32_t n, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                     const void* q_weight, const void* k_weight, float eps, const float* rope,
+                     int64_t n_pos, int32_t rope_dim, int32_t interleaved, const int32_t* pos,
+                     void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride,
+                     hipStream_t stream);
+
+/*
+ * Pages and cache rows of fresh tokens, from the sequences' lengths alone. Sequence s has
+ * past[s] rows in the cache (clamped to [0, R], R = max_pages * page_size) and gets fresh[s] more
+ * (at least 0), whose tokens are packed: sequence by sequence, at most n_tokens
+ * of them, and what is beyond that does not count as fresh. New pages come from the
+ * ring free_pages[n_free], sequence by sequence: free_at[0] is the entry that holds the first free
+ * page and free_at[1] how many are free.
+ *   cu         int32 [n_seqs + 1]: first packed token of each sequence, and their count
+ *   kv_lens    int32 [n_seqs]: past + fresh, at most R
+ *   page_table int32 [n_seqs, max_pages]: entry i of sequence s with ceil(past / page_size)
+ *              <= i < ceil(kv_lens / page_size) becomes the next free page, or -1 when there is none
+ *              left. Other entries are kept
+ *   pos        int32 [n_tokens]: position of the token in its sequence; -1 behind the last
+ *   slots      int32 [n_tokens]: its cache row (hsa_cache_store's idx); -1 behind the last token, past
+ *              R, in a page whose entry is negative, and for a row that does not fit int32
+ *   free_next  int32 [3]: free_at after the call, and in [2] the pages that were lacking
+ * free_at[0] is taken modulo n_free, free_at[1] clamped to [0, n_free]. A page goes back to the ring as
+ * entry (free_at[0] + free_at[1]) % n_free, with free_at[1] one more. kv_lens may be past and
+ * free_next free_at: then the next call goes on from there (a second kernel writes them). The other outputs
+ * must not overlap an input or each other. R <= 2^30, n_free <= 2^30, n_tokens < 2^30.
+ */
+int hsa_page_plan(const int32_t* past, const int32_t* fresh, int32_t n_seqs, int32_t page_size,
+                  int32_t max_pages, int32_t* page_table, const int32_t* free_pages,
+                  int32_t n_free, const int32_t* free_at, int32_t n_tokens, int32_t* cu,
+                  int32_t* kv_lens, int32_t* pos, int32_t* slots, int32_t* free_next,
+                  hipStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -1,4 +1,4 @@
-// Cache rows in 8 bits: written by row index as they are quantized, and read
+// Cache rows in 8 or 4 bits: written by row index as they are quantized, and read
 // back. Both are streams: 8 values per thread and tensor, 16 bytes of bf16.
 //
 //   store  amax over a row's head (head_dim / 8 neighbouring lanes, three or four DPP
@@ -7,6 +7,10 @@
 //          values the same order), so one packed maximum serves two bf16 values, and
 //          whatever is not finite is found by the same comparison.
 //   load   code * 2^e, exact in bf16 and fp32.
+// In 4 bits (e2m1) the exponent is that of 32 values, four lanes, with 6 in the place of
+// 448; a group with a value that is not finite is marked by its exponent. The conversion
+// from fp32 rounds to nearest even and saturates, that to bf16 or fp32 takes the
+// exponent as an operand.
 #include "seq_common.h"
 
 namespace hsa {
@@ -138,6 +142,41 @@ __device__ __forceinline__ u32x2 quantize(const Vals<BF16>& v, int& e) {
   return c;
 }
 
+// e2m1 codes of 8 values, and their group's exponent (the same in its 4 lanes)
+template <bool BF16>
+__device__ __forceinline__ unsigned quantize4(const Vals<BF16>& v, int& e) {
+  unsigned m = v.top();
+  m = max(m, dpp<0xB1>(m));  // lane ^ 1
+  m = max(m, dpp<0x4E>(m));  // lane ^ 2
+  // 6 = 1.5 * 2^2: the next exponent up where the fraction is above 1.5
+  e = min(max((int)((m + 0x3fffffu) >> 23) - 2 - 127, kExp4Min), kExp4Max);
+  const float inv = pow2(-e);
+  if (m >= 0x7f800000u) e = kExp4Nan;
+  unsigned c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v.at(0) * inv, v.at(1) * inv, 1.f, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v.at(2) * inv, v.at(3) * inv, 1.f, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v.at(4) * inv, v.at(5) * inv, 1.f, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v.at(6) * inv, v.at(7) * inv, 1.f, 3);
+}
+
+template <bool BF16>
+__device__ __forceinline__ Vals<BF16> values4(unsigned c, int e) {
+  const float s = pow2(e);
+  Vals<BF16> v;
+  if constexpr (BF16) {
+    v.x[0] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
+    v.x[1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
+    v.x[2] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
+    v.x[3] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
+  } else {
+    const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1);
+    const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2), f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3);
+    v.x[0] = (f32x4){a[0], a[1], b[0], b[1]};
+    v.x[1] = (f32x4){d[0], d[1], f[0], f[1]};
+  }
+  return v;
+}
+
 template <bool BF16>
 __device__ __forceinline__ Vals<BF16> values(u32x2 c, int e) {
   const float s = pow2(e);
@@ -166,7 +205,7 @@ struct Place {
   }
 };
 
-template <bool BF16, int DH, bool E4M3>
+template <bool BF16, int DH, Held HELD>
 __global__ __launch_bounds__(kThreads) void store_kernel(CacheRows c, FastDiv chunks) {
   const Place p(chunks);
   Vals<BF16> kx, vx;
@@ -180,7 +219,17 @@ __global__ __launch_bounds__(kThreads) void store_kernel(CacheRows c, FastDiv ch
     if (t >= 0 && t < c.n_rows) dst = t;
   }
   const long at = dst * (long)(chunks.d * 8) + p.col;
-  if constexpr (E4M3) {
+  if constexpr (HELD == kE2M1) {
+    int ke, ve;
+    const unsigned kc = quantize4<BF16>(kx, ke), vc = quantize4<BF16>(vx, ve);
+    if (dst < 0) return;
+    put<true>(kc, static_cast<char*>(c.dst_k) + at / 2);
+    put<true>(vc, static_cast<char*>(c.dst_v) + at / 2);
+    if (p.col % kGroup == 0) {
+      c.k_exp[at / kGroup] = (int8_t)ke;
+      c.v_exp[at / kGroup] = (int8_t)ve;
+    }
+  } else if constexpr (HELD == kE4M3) {
     int ke, ve;
     const u32x2 kc = quantize<BF16, DH>(kx, ke), vc = quantize<BF16, DH>(vx, ve);
     if (dst < 0) return;
@@ -198,7 +247,7 @@ __global__ __launch_bounds__(kThreads) void store_kernel(CacheRows c, FastDiv ch
   }
 }
 
-template <bool BF16, int DH, bool E4M3>
+template <bool BF16, int DH, Held HELD>
 __global__ __launch_bounds__(kThreads) void load_kernel(CacheRows c, FastDiv chunks) {
   const Place p(chunks);
   if (p.row >= c.n) return;
@@ -208,7 +257,12 @@ __global__ __launch_bounds__(kThreads) void load_kernel(CacheRows c, FastDiv chu
   const int t = c.idx[p.row];
   if (t >= 0 && t < c.n_rows) {
     const long at = (long)t * (long)(chunks.d * 8) + p.col;
-    if constexpr (E4M3) {
+    if constexpr (HELD == kE2M1) {
+      const unsigned kc = get<unsigned>(static_cast<const char*>(c.src_k) + at / 2);
+      const unsigned vc = get<unsigned>(static_cast<const char*>(c.src_v) + at / 2);
+      kx = values4<BF16>(kc, c.k_exp[at / kGroup]);
+      vx = values4<BF16>(vc, c.v_exp[at / kGroup]);
+    } else if constexpr (HELD == kE4M3) {
       const u32x2 kc = get<u32x2>(static_cast<const char*>(c.src_k) + at);
       const u32x2 vc = get<u32x2>(static_cast<const char*>(c.src_v) + at);
       const long h = (long)t * c.kv_heads + p.col / DH;
@@ -224,20 +278,36 @@ __global__ __launch_bounds__(kThreads) void load_kernel(CacheRows c, FastDiv chu
   vx.template store<false>(c.dst_v, p.row * c.v_stride + p.col);
 }
 
-template <bool STORE, bool BF16, int DH, bool E4M3>
+template <bool BF16>
+__global__ __launch_bounds__(kThreads) void quantize_w4_kernel(const void* w, long n, long stride, char* codes,
+                                                               int8_t* exps, FastDiv chunks) {
+  const Place p(chunks);
+  Vals<BF16> x;
+  x.zero();
+  if (p.row < n) x.load(w, p.row * stride + p.col);
+  int e;
+  const unsigned c = quantize4<BF16>(x, e);
+  if (p.row >= n) return;
+  const long at = p.row * (long)(chunks.d * 8) + p.col;
+  put<true>(c, codes + at / 2);
+  if (p.col % kGroup == 0) exps[at / kGroup] = (int8_t)e;
+}
+
+template <bool STORE, bool BF16, int DH, Held HELD>
 hipError_t launch(const CacheRows& c, hipStream_t s) {
   const uint32_t chunks = (uint32_t)c.kv_heads * (DH / 8);  // of a row
   const long groups = ((long)c.n * chunks + kThreads - 1) / kThreads;
   if constexpr (STORE)
-    hipLaunchKernelGGL((store_kernel<BF16, DH, E4M3>), dim3((unsigned)groups), dim3(kThreads), 0, s, c, FastDiv(chunks));
+    hipLaunchKernelGGL((store_kernel<BF16, DH, HELD>), dim3((unsigned)groups), dim3(kThreads), 0, s, c, FastDiv(chunks));
   else
-    hipLaunchKernelGGL((load_kernel<BF16, DH, E4M3>), dim3((unsigned)groups), dim3(kThreads), 0, s, c, FastDiv(chunks));
+    hipLaunchKernelGGL((load_kernel<BF16, DH, HELD>), dim3((unsigned)groups), dim3(kThreads), 0, s, c, FastDiv(chunks));
   return hipGetLastError();
 }
 
 template <bool STORE, bool BF16, int DH>
 hipError_t launch_held(const CacheRows& c, hipStream_t s) {
-  return c.e4m3 ? launch<STORE, BF16, DH, true>(c, s) : launch<STORE, BF16, DH, false>(c, s);
+  if (c.held == kE2M1) return launch<STORE, BF16, DH, kE2M1>(c, s);
+  return c.held == kE4M3 ? launch<STORE, BF16, DH, kE4M3>(c, s) : launch<STORE, BF16, DH, kOwn>(c, s);
 }
 
 template <bool STORE>
@@ -251,5 +321,18 @@ hipError_t launch_any(const CacheRows& c, hipStream_t s) {
 
 hipError_t launch_cache_store(const CacheRows& c, hipStream_t s) { return launch_any<true>(c, s); }
 hipError_t launch_cache_load(const CacheRows& c, hipStream_t s) { return launch_any<false>(c, s); }
+
+hipError_t launch_quantize_w4(const void* w, bool bf16, long n, int d, long stride, void* codes, int8_t* exps,
+                              hipStream_t s) {
+  if (n <= 0) return hipSuccess;
+  const uint32_t chunks = (uint32_t)d / 8;
+  const unsigned groups = (unsigned)((n * chunks + kThreads - 1) / kThreads);
+  char* c = static_cast<char*>(codes);
+  if (bf16)
+    hipLaunchKernelGGL(quantize_w4_kernel<true>, dim3(groups), dim3(kThreads), 0, s, w, n, stride, c, exps, FastDiv(chunks));
+  else
+    hipLaunchKernelGGL(quantize_w4_kernel<false>, dim3(groups), dim3(kThreads), 0, s, w, n, stride, c, exps, FastDiv(chunks));
+  return hipGetLastError();
+}
 
 }  // namespace hsa

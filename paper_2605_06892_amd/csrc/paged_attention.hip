@@ -141,33 +141,39 @@ __device__ __forceinline__ void write_out(const PagedArgs& a, long orow, int c, 
 }
 
 // One item, or the rows key0 .. key1-1 of one, by NW waves.
-template <bool F32, bool E4M3, int DH, bool ALIGNED, int NW>
+template <bool F32, Held HELD, int DH, bool ALIGNED, int NW>
 struct Attend {
+  static constexpr bool E4M3 = HELD == kE4M3, E2M1 = HELD == kE2M1, EXPS = E4M3 || E2M1;
+  static constexpr bool VREG = F32 || E2M1;       // V goes from its loads to the products without LDS
   static constexpr int BK = F32 ? 16 : 32;        // keys per block
   static constexpr int KT = BK / 16;              // key tiles of a block
   static constexpr int DT = DH / 16;              // channel tiles of O^T
   static constexpr int P = DH + 4;                // padded row of the merge buffer, floats
-  static constexpr int ES = E4M3 ? 1 : (F32 ? 4 : 2);
-  static constexpr int CB = 16;                   // bytes of a load
-  static constexpr int CE = CB / ES;              // values of a load
+  static constexpr int BITS = E2M1 ? 4 : E4M3 ? 8 : (F32 ? 32 : 16);
+  static constexpr int HB = DH * BITS / 8;        // bytes of a head's row
+  static constexpr int HX = E2M1 ? DH / kGroup : 1;  // its exponents
+  static constexpr int CB = E2M1 ? HB / 4 : 16;   // bytes of a load
+  static constexpr int CE = CB * 8 / BITS;        // values of a load
   static constexpr int KL = DH / CE / 4;          // K loads per lane and key tile (its 4 slots share a row)
-  // V: bf16 form, whole rows over the wave; fp32 form, DT consecutive channels of the 4 keys of a slot
-  static constexpr int VR = F32 ? 4 : BK * DH / CE / 64;
-  static constexpr int VB = F32 ? DT * ES : CB;   // bytes of one V read
+  // V: in the bf16 form whole rows over the wave; where it stays in registers DT consecutive
+  // channels of the keys of a slot (4 of each key tile)
+  static constexpr int VR = VREG ? 4 * KT : BK * DH / CE / 64;
+  static constexpr int VB = VREG ? DT * BITS / 8 : CB;  // bytes of one V read
   static constexpr int CPR = DH / CE;             // loads per row
   static constexpr unsigned kAll = BK == 32 ? ~0u : 0xffffu;
   struct VLoad { unsigned char b[VB]; };
+  struct KLoad { unsigned w[CB / 4]; };
   struct Shared {
     float buf[NW][kRows * P];  // V rows, then the merge
     float m_part[NW][kRows], l_part[NW][kRows];
   };
-  static_assert(F32 || kRows * P * 4 >= BK * DH * 2, "a block's V rows fit");
+  static_assert(VREG || kRows * P * 4 >= BK * DH * 2, "a block's V rows fit");
 
   // The bf16 form loads whole rows of V, which nothing reads again: past the caches. K, whose rows
   // several loads share, stays (four sequences of 30011 to 131072: 226 us, V past the
   // caches 216, both 238).
   static __device__ __forceinline__ void load_v(VLoad& v, const char* p) {
-    if constexpr (F32) {
+    if constexpr (VREG) {
       __builtin_memcpy(&v, p, VB);
     } else {
       const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
@@ -187,6 +193,19 @@ struct Attend {
     return y;
   }
 
+  // 8 codes of a word as fp32, times a power of two
+  static __device__ __forceinline__ void x8(float (&x)[8], unsigned c, float scale) {
+    const f32x2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0), q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1);
+    const f32x2 r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 2), t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 3);
+    x[0] = p[0], x[1] = p[1], x[2] = q[0], x[3] = q[1], x[4] = r[0], x[5] = r[1], x[6] = t[0], x[7] = t[1];
+  }
+  // 8 codes of a word as bf16, times a power of two: exact
+  static __device__ __forceinline__ bf16x8 widen4(unsigned c, float scale) {
+    const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1);
+    const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2), t = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3);
+    return (bf16x8){p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
+  }
+
   // s, h, g0 (first query head of the group), key0 and key1 are uniform. part:
   // where the unnormalized result goes, NULL for the output itself.
   static __device__ __forceinline__ void run(const PagedArgs& a, const Plan& plan, Shared& sh, int s, int h, int g0,
@@ -194,7 +213,7 @@ struct Attend {
     const int lane = threadIdx.x & 63;
     const int wave = uniform(threadIdx.x >> 6);
     const int l16 = lane & 15, grp = lane >> 4;
-    const unsigned row_bytes = (unsigned)(a.kv_heads * DH) * ES;
+    const unsigned row_bytes = (unsigned)a.kv_heads * HB, row_exps = (unsigned)a.kv_heads * HX;
     const float sl2e = a.scale * kLog2e;
     const int32_t* pages = a.page_table + (long)s * a.max_pages;
     bf16* vl = reinterpret_cast<bf16*>(sh.buf[wave]);
@@ -204,7 +223,7 @@ struct Attend {
 
     // one block ahead: its rows (as held), exponents, and which of its keys exist;
     // two blocks ahead: the page of this lane's key (lane % BK; ALIGNED: of all keys)
-    u32x4 kr[KT][KL];
+    KLoad kr[KT][KL];
     VLoad vr[VR];
     int ke[KT], ve[VR];
     unsigned mask = 0;
@@ -214,10 +233,12 @@ struct Attend {
       page = -1;
       if (t < key1) page = pages[plan.page.quot(t)];
     };
-    auto v_key = [&](int i) { return F32 ? grp * 4 + i : (i * 64 + lane) / CPR; };
+    auto v_key = [&](int i) { return VREG ? grp * 4 + (i & 3) + (i >> 2) * 16 : (i * 64 + lane) / CPR; };
     // byte offsets of this lane's loads in a block's rows, where those are consecutive
     const unsigned k_off = l16 * row_bytes + grp * CB;
-    const unsigned v_off = F32 ? (unsigned)grp * 4 * row_bytes + l16 * VB : (lane / CPR) * row_bytes + lane % CPR * CB;
+    const unsigned v_off = VREG ? (unsigned)grp * 4 * row_bytes + l16 * VB : (lane / CPR) * row_bytes + lane % CPR * CB;
+    // exponents of the channels of this lane's loads
+    const unsigned k_x = E2M1 ? grp * (DH / 4) / kGroup : 0, v_x = E2M1 ? l16 * DT / kGroup : 0;
     auto load = [&](int n0) {
       if (n0 >= key1) return;
       const int t = n0 + (ALIGNED ? 0 : lane % BK);
@@ -227,37 +248,37 @@ struct Attend {
       if constexpr (ALIGNED) {  // a block lies in one page: rows first ..
         first = uniform(first);
         load_page(n0 + NW * BK);
-        const char* kb = static_cast<const char*>(a.k) + (long)first * row_bytes + h * (DH * ES);
-        const char* vb = static_cast<const char*>(a.v) + (long)first * row_bytes + h * (DH * ES);
-        const int8_t* keb = a.k_exp + (long)first * a.kv_heads + h;
-        const int8_t* veb = a.v_exp + (long)first * a.kv_heads + h;
+        const char* kb = static_cast<const char*>(a.k) + (long)first * row_bytes + h * HB;
+        const char* vb = static_cast<const char*>(a.v) + (long)first * row_bytes + h * HB;
+        const int8_t* keb = a.k_exp + (long)first * row_exps + h * HX;
+        const int8_t* veb = a.v_exp + (long)first * row_exps + h * HX;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
 #pragma unroll
           for (int i = 0; i < KL; ++i) __builtin_memcpy(&kr[kt][i], kb + (kt * 16 * row_bytes + k_off + i * 4 * CB), CB);
-          if constexpr (E4M3) ke[kt] = keb[(unsigned)(kt * 16 + l16) * a.kv_heads];
+          if constexpr (EXPS) ke[kt] = keb[(unsigned)(kt * 16 + l16) * row_exps + k_x];
         }
 #pragma unroll
         for (int i = 0; i < VR; ++i) {
-          load_v(vr[i], vb + ((F32 ? i : i * 64 / CPR) * row_bytes + v_off));
-          if constexpr (E4M3) ve[i] = veb[(unsigned)v_key(i) * a.kv_heads];
+          load_v(vr[i], vb + ((VREG ? (i & 3) + (i >> 2) * 16 : i * 64 / CPR) * row_bytes + v_off));
+          if constexpr (EXPS) ve[i] = veb[(unsigned)v_key(i) * row_exps + v_x];
         }
       } else {
         load_page(n0 + NW * BK);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
           const long r = __shfl(first, kt * 16 + l16);
-          const char* src = static_cast<const char*>(a.k) + r * row_bytes + h * (DH * ES) + grp * CB;
+          const char* src = static_cast<const char*>(a.k) + r * row_bytes + h * HB + grp * CB;
 #pragma unroll
           for (int i = 0; i < KL; ++i) __builtin_memcpy(&kr[kt][i], src + i * 4 * CB, CB);
-          if constexpr (E4M3) ke[kt] = a.k_exp[r * a.kv_heads + h];
+          if constexpr (EXPS) ke[kt] = a.k_exp[r * row_exps + h * HX + k_x];
         }
 #pragma unroll
         for (int i = 0; i < VR; ++i) {
           const long r = __shfl(first, v_key(i));
-          const unsigned c = F32 ? l16 * VB : lane % CPR * CB;
-          load_v(vr[i], static_cast<const char*>(a.v) + r * row_bytes + h * (DH * ES) + c);
-          if constexpr (E4M3) ve[i] = a.v_exp[r * a.kv_heads + h];
+          const unsigned c = VREG ? l16 * VB : lane % CPR * CB;
+          load_v(vr[i], static_cast<const char*>(a.v) + r * row_bytes + h * HB + c);
+          if constexpr (EXPS) ve[i] = a.v_exp[r * row_exps + h * HX + v_x];
         }
       }
     };
@@ -297,25 +318,35 @@ struct Attend {
       float vf[F32 ? 4 : 1][DT];
       if constexpr (F32) {
         // codes times their exponent before the products, which could overflow without it
-        const float sk = E4M3 ? pow2(ke[0]) : 1.f;
+        const float sk = EXPS ? pow2(ke[0]) : 1.f;
 #pragma unroll
         for (int i = 0; i < KL; ++i)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            float x[CE / 4];
-            if constexpr (E4M3) {
-              const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)kr[0][i][j], false);
-              const f32x2 up = __builtin_amdgcn_cvt_pk_f32_fp8((int)kr[0][i][j], true);
+          for (int j = 0; j < CB / 4; ++j) {
+            constexpr int N = 32 / BITS;  // values of a word
+            float x[N];
+            if constexpr (E2M1) {
+              x8(x, kr[0][i].w[j], sk);
+            } else if constexpr (E4M3) {
+              const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)kr[0][i].w[j], false);
+              const f32x2 up = __builtin_amdgcn_cvt_pk_f32_fp8((int)kr[0][i].w[j], true);
               x[0] = lo[0] * sk, x[1] = lo[1] * sk, x[2] = up[0] * sk, x[3] = up[1] * sk;
             } else {
-              x[0] = __uint_as_float(kr[0][i][j]);
+              x[0] = __uint_as_float(kr[0][i].w[j]);
             }
 #pragma unroll
-            for (int u = 0; u < CE / 4; ++u) sc[0] = Mfma<16>::mul(x[u], qs[i * CE + j * (CE / 4) + u], sc[0]);
+            for (int u = 0; u < N; ++u) sc[0] = Mfma<16>::mul(x[u], qs[i * CE + j * N + u], sc[0]);
           }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if constexpr (E4M3) {
+          if constexpr (E2M1) {
+            unsigned c = 0;
+            __builtin_memcpy(&c, &vr[i], VB);
+            float x[8];
+            x8(x, c, pow2(ve[i]));
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) vf[i][dt] = x[dt];
+          } else if constexpr (E4M3) {
             const float sv = pow2(ve[i]);
 #pragma unroll
             for (int j = 0; j < DT / 4; ++j) {
@@ -334,6 +365,7 @@ struct Attend {
             for (int dt = 0; dt < DT; ++dt) vf[i][dt] = 0.f;
         }
       } else {
+        if constexpr (!VREG)
 #pragma unroll
         for (int i = 0; i < VR; ++i) {
           const int f = i * 64 + lane, r = f / CPR;
@@ -355,17 +387,40 @@ struct Attend {
         for (int i = 0; i < KL; ++i)
 #pragma unroll
           for (int kt = 0; kt < KT; ++kt) {
-            if constexpr (E4M3) {
+            if constexpr (E2M1) {
+              const float sk = pow2(ke[kt]);
+#pragma unroll
+              for (int j = 0; j < CB / 4; ++j)
+                sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen4(kr[kt][i].w[j], sk), qb[i * (CE / 8) + j], sc[kt], 0, 0, 0);
+            } else if constexpr (E4M3) {
               const float sk = pow2(ke[kt]);
 #pragma unroll
               for (int j = 0; j < 2; ++j)
-                sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(kr[kt][i][2 * j], kr[kt][i][2 * j + 1], sk),
+                sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(kr[kt][i].w[2 * j], kr[kt][i].w[2 * j + 1], sk),
                                                                  qb[i * 2 + j], sc[kt], 0, 0, 0);
             } else {
               sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[kt][i]), qb[i], sc[kt], 0, 0, 0);
             }
           }
-        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");  // the V rows are in LDS
+        if constexpr (!VREG) __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");  // the V rows are in LDS
+      }
+      // V of the slot's 8 keys, two channels of a tile pair each
+      bf16x2 v2[E2M1 && !F32 ? DT / 2 : 1][8];
+      if constexpr (E2M1 && !F32) {
+#pragma unroll
+        for (int i = 0; i < VR; ++i) {
+          unsigned c = 0;
+          __builtin_memcpy(&c, &vr[i], VB);
+          int e = ve[i];
+          if (cut && !(keys >> v_key(i) & 1)) c = 0, e = 0;  // neither codes nor exponents of rows that are not there
+          const float sv = pow2(e);
+          v2[0][i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, sv, 0);
+          v2[1][i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, sv, 1);
+          if constexpr (DT == 8) {
+            v2[2][i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, sv, 2);
+            v2[3][i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, sv, 3);
+          }
+        }
       }
       load(n0 + NW * BK);
 
@@ -407,6 +462,15 @@ struct Attend {
       } else {
         const bf16x8 pf = __builtin_shufflevector(to_bf16x4(sc[0]), to_bf16x4(sc[KT - 1]), 0, 1, 2, 3, 4, 5, 6, 7);
         const int r = grp * 4 + (l16 >> 2);
+        if constexpr (E2M1) {
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt) {
+            bf16x8 vf8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) vf8[i] = v2[dt / 2][i][dt & 1];
+            acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf8, pf, acc[dt], 0, 0, 0);
+          }
+        } else
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
           const int col = dt * 16 + 4 * (lane & 3);
@@ -416,12 +480,12 @@ struct Attend {
           acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7), pf,
                                                             acc[dt], 0, 0, 0);
         }
-        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");  // read before the next block's rows
+        if constexpr (!VREG) __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");  // read before the next block's rows
       }
     }
 
     // merge of the waves. acc[dt][e] is channel dt*16 + grp*4 + e of row l16,
-    // in the fp32 form (grp*4 + e)*DT + dt
+    // where V stays in registers (grp*4 + e)*DT + dt
     float l_tot = l_run + __shfl_xor(l_run, 16);
     l_tot += __shfl_xor(l_tot, 32);
     if (grp == 0) {
@@ -430,7 +494,7 @@ struct Attend {
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      if constexpr (F32) {
+      if constexpr (VREG) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) sh.buf[wave][l16 * P + (grp * 4 + e) * DT + dt] = acc[dt][e];
       } else {
@@ -465,9 +529,9 @@ struct Attend {
 };
 
 // one item per workgroup
-template <bool F32, bool E4M3, int DH, bool ALIGNED>
+template <bool F32, Held HELD, int DH, bool ALIGNED>
 __global__ __launch_bounds__(kWholeWaves * 64) void paged_whole_kernel(PagedArgs a, Plan plan) {
-  typedef Attend<F32, E4M3, DH, ALIGNED, kWholeWaves> A;
+  typedef Attend<F32, HELD, DH, ALIGNED, kWholeWaves> A;
   __shared__ __attribute__((aligned(16))) typename A::Shared sh;
   const int per = a.kv_heads * plan.gts;
   const int s = blockIdx.x / per, item = blockIdx.x - s * per, h = item / plan.gts;
@@ -477,9 +541,9 @@ __global__ __launch_bounds__(kWholeWaves * 64) void paged_whole_kernel(PagedArgs
 // One run of tiles per workgroup. Two waves to a SIMD, stated: without it the
 // compiler spreads the 128-wide forms over more registers than that leaves (48
 // sequences of 201 to 8009 rows in bf16 94 -> 85 us).
-template <bool F32, bool E4M3, int DH, bool ALIGNED>
+template <bool F32, Held HELD, int DH, bool ALIGNED>
 __global__ __launch_bounds__(kSplitWaves * 64, 2) void paged_split_kernel(PagedArgs a, Plan plan) {
-  typedef Attend<F32, E4M3, DH, ALIGNED, kSplitWaves> A;
+  typedef Attend<F32, HELD, DH, ALIGNED, kSplitWaves> A;
   __shared__ __attribute__((aligned(16))) typename A::Shared sh;
   const int per = a.kv_heads * plan.gts;
   Walk walk;
@@ -591,17 +655,17 @@ int workgroups(int n_seqs, int kv_heads, int group, long max_len) {
   return (int)std::min(std::min((long)kMaxGroups, 2L * compute_units()), tiles);
 }
 
-template <bool F32, bool E4M3, int DH, bool ALIGNED>
+template <bool F32, Held HELD, int DH, bool ALIGNED>
 hipError_t launch(const PagedArgs& a, hipStream_t s) {
   const long max_len = (long)a.max_pages * a.page_size;
   Plan plan{0, gts_of(a.group), FastDiv((uint32_t)a.page_size)};
   if (!splits(a.n_seqs, a.kv_heads, a.group, max_len)) {
-    hipLaunchKernelGGL((paged_whole_kernel<F32, E4M3, DH, ALIGNED>), dim3((unsigned)(a.n_seqs * a.kv_heads * plan.gts)),
+    hipLaunchKernelGGL((paged_whole_kernel<F32, HELD, DH, ALIGNED>), dim3((unsigned)(a.n_seqs * a.kv_heads * plan.gts)),
                        dim3(kWholeWaves * 64), 0, s, a, plan);
     return hipGetLastError();
   }
   plan.wgs = workgroups(a.n_seqs, a.kv_heads, a.group, max_len);
-  hipLaunchKernelGGL((paged_split_kernel<F32, E4M3, DH, ALIGNED>), dim3(plan.wgs), dim3(kSplitWaves * 64), 0, s, a, plan);
+  hipLaunchKernelGGL((paged_split_kernel<F32, HELD, DH, ALIGNED>), dim3(plan.wgs), dim3(kSplitWaves * 64), 0, s, a, plan);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((paged_join_kernel<F32, DH>), dim3(plan.wgs, std::min(a.group, kRows)), dim3(kJoinThreads), 0, s, a, plan);
@@ -609,10 +673,12 @@ hipError_t launch(const PagedArgs& a, hipStream_t s) {
 }
 
 template <bool F32, int DH>
-hipError_t launch_held(const PagedArgs& a, bool e4m3, hipStream_t s) {
+hipError_t launch_held(const PagedArgs& a, Held held, hipStream_t s) {
   // a block of 32 rows lies in one page where the page size is a multiple of 32
-  if (a.page_size % 32 == 0) return e4m3 ? launch<F32, true, DH, true>(a, s) : launch<F32, false, DH, true>(a, s);
-  return e4m3 ? launch<F32, true, DH, false>(a, s) : launch<F32, false, DH, false>(a, s);
+  const bool whole = a.page_size % 32 == 0;
+  if (held == kE2M1) return whole ? launch<F32, kE2M1, DH, true>(a, s) : launch<F32, kE2M1, DH, false>(a, s);
+  if (held == kE4M3) return whole ? launch<F32, kE4M3, DH, true>(a, s) : launch<F32, kE4M3, DH, false>(a, s);
+  return whole ? launch<F32, kOwn, DH, true>(a, s) : launch<F32, kOwn, DH, false>(a, s);
 }
 
 }  // namespace
@@ -624,10 +690,10 @@ size_t paged_attention_bytes(int n_seqs, int kv_heads, int group, int head_dim, 
   return (size_t)workgroups(n_seqs, kv_heads, group, max_len) * (2 * kRows * (head_dim + 2) * sizeof(float) + sizeof(Note));
 }
 
-hipError_t launch_paged_attention(const PagedArgs& a, bool bf16, bool e4m3, int head_dim, hipStream_t s) {
+hipError_t launch_paged_attention(const PagedArgs& a, bool bf16, Held held, int head_dim, hipStream_t s) {
   if (a.n_seqs <= 0) return hipSuccess;
-  if (bf16) return head_dim == 64 ? launch_held<false, 64>(a, e4m3, s) : launch_held<false, 128>(a, e4m3, s);
-  return head_dim == 64 ? launch_held<true, 64>(a, e4m3, s) : launch_held<true, 128>(a, e4m3, s);
+  if (bf16) return head_dim == 64 ? launch_held<false, 64>(a, held, s) : launch_held<false, 128>(a, held, s);
+  return head_dim == 64 ? launch_held<true, 64>(a, held, s) : launch_held<true, 128>(a, held, s);
 }
 
 }  // namespace hsa

@@ -44,10 +44,21 @@ bool any_overlap(const Range (&r)[N], int outs) {
   return false;
 }
 
-// The cache's element size; 0 unless cache_dtype is dtype or e4m3.
-size_t cache_elem(int dtype, int cache_dtype) {
-  if (cache_dtype == HSA_STEP_E4M3) return 1;
-  return cache_dtype == dtype ? elem_size(dtype) : 0;
+// How a cache holds rows of kv_heads heads: the bytes of a row (0 unless cache_dtype is
+// dtype or a type of codes), its exponents, and the alignment of its first row.
+struct HeldRow {
+  hsa::Held held;
+  size_t bytes, exps, align;
+};
+HeldRow held_row(int dtype, int cache_dtype, int64_t kv_heads, int64_t head_dim) {
+  const size_t d = (size_t)(kv_heads * head_dim);
+  if (cache_dtype == HSA_STEP_E4M3) return {hsa::kE4M3, d, (size_t)kv_heads, 16};
+  if (cache_dtype == HSA_STEP_E2M1) return {hsa::kE2M1, d / 2, d / hsa::kGroup, 16};
+  const size_t es = cache_dtype == dtype ? elem_size(dtype) : 0;
+  return {hsa::kOwn, d * es, 0, es == 4 ? size_t(4) : size_t(16)};
+}
+bool cache_dtype_ok(int dtype, int cache_dtype) {
+  return elem_size(dtype) && (cache_dtype == dtype || cache_dtype == HSA_STEP_E4M3 || cache_dtype == HSA_STEP_E2M1);
 }
 
 // Checks of hsa_cache_store and hsa_cache_load that do not depend on the direction.
@@ -55,19 +66,18 @@ int check_cache(int dtype, const void* k, int64_t k_stride, const void* v, int64
                 const int32_t* idx, int32_t n, int64_t n_rows, int32_t kv_heads, int32_t head_dim,
                 int cache_dtype, const void* k_cache, const void* v_cache, const int8_t* k_exp,
                 const int8_t* v_exp) {
-  const size_t es = elem_size(dtype), ce = cache_elem(dtype, cache_dtype);
-  if (!es || !ce) return HSA_STEP_ERR_DTYPE;
+  if (!cache_dtype_ok(dtype, cache_dtype)) return HSA_STEP_ERR_DTYPE;
+  const size_t es = elem_size(dtype);
   if (n < 0 || n_rows < 0 || n_rows > kMaxRows || !heads_ok(kv_heads, kv_heads, head_dim)) return HSA_STEP_ERR_SHAPE;
   const int64_t d = (int64_t)kv_heads * head_dim;
+  const HeldRow row = held_row(dtype, cache_dtype, kv_heads, head_dim);
   // one launch: fewer than 2^32 threads of 8 values
-  if (!fits(n_rows, d, ce) || (int64_t)n * d >= kMaxLaunch * 4) return HSA_STEP_ERR_SHAPE;
+  if (!fits(n_rows, (int64_t)row.bytes) || (int64_t)n * d >= kMaxLaunch * 4) return HSA_STEP_ERR_SHAPE;
   if (n == 0) return HSA_STEP_OK;
   if (!k || !v || !idx || (n_rows > 0 && (!k_cache || !v_cache))) return HSA_STEP_ERR_NULL;
-  const bool exps = cache_dtype == HSA_STEP_E4M3;
-  if (exps && n_rows > 0 && (!k_exp || !v_exp)) return HSA_STEP_ERR_NULL;
-  const size_t ca = ce == 4 ? 4 : 16;
+  if (row.exps && n_rows > 0 && (!k_exp || !v_exp)) return HSA_STEP_ERR_NULL;
   if (!rows_ok(k, n, k_stride, d, es) || !rows_ok(v, n, v_stride, d, es) || !aligned(idx, 4) ||
-      !aligned(k_cache, ca) || !aligned(v_cache, ca))
+      !aligned(k_cache, row.align) || !aligned(v_cache, row.align))
     return HSA_STEP_ERR_SHAPE;
   return HSA_STEP_OK;
 }
@@ -82,9 +92,8 @@ HSA_API int hsa_cache_store(int dtype, const void* k, int64_t k_stride, const vo
                              cache_dtype, k_cache, v_cache, k_exp, v_exp);
   if (st != HSA_STEP_OK || n == 0) return st;
   const int64_t d = (int64_t)kv_heads * head_dim;
-  const bool e4m3 = cache_dtype == HSA_STEP_E4M3;
-  const size_t cb = (size_t)n_rows * d * cache_elem(dtype, cache_dtype);
-  const size_t eb = e4m3 ? (size_t)n_rows * kv_heads : 0;
+  const HeldRow row = held_row(dtype, cache_dtype, kv_heads, head_dim);
+  const size_t cb = (size_t)n_rows * row.bytes, eb = (size_t)n_rows * row.exps;
   const size_t es = elem_size(dtype);
   const Range r[] = {{k_cache, cb}, {v_cache, cb}, {k_exp, eb}, {v_exp, eb}, {k, span(n, k_stride, d, es)},
                      {v, span(n, v_stride, d, es)}, {idx, (size_t)n * 4}};
@@ -92,7 +101,7 @@ HSA_API int hsa_cache_store(int dtype, const void* k, int64_t k_stride, const vo
   if (n_rows == 0) return HSA_STEP_OK;
   hsa::CacheRows c{};
   c.bf16 = dtype == HSA_STEP_BF16;
-  c.e4m3 = e4m3;
+  c.held = row.held;
   c.src_k = k;
   c.src_v = v;
   c.dst_k = k_cache;
@@ -117,16 +126,15 @@ HSA_API int hsa_cache_load(int cache_dtype, const void* k_cache, const void* v_c
                              cache_dtype, k_cache, v_cache, k_exp, v_exp);
   if (st != HSA_STEP_OK || n == 0) return st;
   const int64_t d = (int64_t)kv_heads * head_dim;
-  const bool e4m3 = cache_dtype == HSA_STEP_E4M3;
-  const size_t cb = (size_t)n_rows * d * cache_elem(dtype, cache_dtype);
-  const size_t eb = e4m3 ? (size_t)n_rows * kv_heads : 0;
+  const HeldRow row = held_row(dtype, cache_dtype, kv_heads, head_dim);
+  const size_t cb = (size_t)n_rows * row.bytes, eb = (size_t)n_rows * row.exps;
   const size_t es = elem_size(dtype);
   const Range r[] = {{k, span(n, k_stride, d, es)}, {v, span(n, v_stride, d, es)}, {k_cache, cb}, {v_cache, cb},
                      {k_exp, eb}, {v_exp, eb}, {idx, (size_t)n * 4}};
   if (any_overlap(r, 2)) return HSA_STEP_ERR_ALIAS;
   hsa::CacheRows c{};
   c.bf16 = dtype == HSA_STEP_BF16;
-  c.e4m3 = e4m3;
+  c.held = row.held;
   c.src_k = k_cache;
   c.src_v = v_cache;
   c.dst_k = k;
@@ -204,30 +212,29 @@ HSA_API int hsa_paged_attention(int dtype, const void* q, int64_t q_stride, int 
                                 int32_t page_size, int32_t heads, int32_t kv_heads,
                                 int32_t head_dim, float scale, void* o, float* lse,
                                 void* workspace, size_t workspace_bytes, hipStream_t stream) {
-  const size_t es = elem_size(dtype), ce = cache_elem(dtype, cache_dtype);
-  if (!es || !ce) return HSA_STEP_ERR_DTYPE;
+  if (!cache_dtype_ok(dtype, cache_dtype)) return HSA_STEP_ERR_DTYPE;
+  const size_t es = elem_size(dtype);
   if (!heads_ok(heads, kv_heads, head_dim) || n_seqs < 0 || n_seqs > kMaxRows / heads || n_pages < 0 ||
       max_pages < 0 || page_size < 1 || (int64_t)n_pages * page_size > kMaxRows ||
       (int64_t)max_pages * page_size > kMaxKeys || !scale_ok(scale))
     return HSA_STEP_ERR_SHAPE;
-  const int64_t d = (int64_t)heads * head_dim, dk = (int64_t)kv_heads * head_dim;
+  const int64_t d = (int64_t)heads * head_dim;
+  const HeldRow row = held_row(dtype, cache_dtype, kv_heads, head_dim);
   const int64_t n_rows = (int64_t)n_pages * page_size;
-  if (!fits(n_rows, dk, ce) || !fits(n_seqs, max_pages, 4) || (int64_t)n_seqs * heads >= kMaxLaunch / 512)
+  if (!fits(n_rows, (int64_t)row.bytes) || !fits(n_seqs, max_pages, 4) || (int64_t)n_seqs * heads >= kMaxLaunch / 512)
     return HSA_STEP_ERR_SHAPE;
   if (n_seqs == 0) return HSA_STEP_OK;
-  const bool e4m3 = cache_dtype == HSA_STEP_E4M3;
   if (!q || !kv_lens || !o || (max_pages > 0 && !page_table) || (n_rows > 0 && (!k_cache || !v_cache)) ||
-      (e4m3 && n_rows > 0 && (!k_exp || !v_exp)))
+      (row.exps && n_rows > 0 && (!k_exp || !v_exp)))
     return HSA_STEP_ERR_NULL;
-  const size_t ca = ce == 4 ? 4 : 16;
-  if (!rows_ok(q, n_seqs, q_stride, d, es) || !aligned(k_cache, ca) || !aligned(v_cache, ca) ||
+  if (!rows_ok(q, n_seqs, q_stride, d, es) || !aligned(k_cache, row.align) || !aligned(v_cache, row.align) ||
       !aligned(o, es == 2 ? 16 : 4) || !aligned(lse, 4) || !aligned(page_table, 4) || !aligned(kv_lens, 4))
     return HSA_STEP_ERR_SHAPE;
   const size_t need = hsa_paged_attention_workspace_bytes(dtype, n_seqs, heads, kv_heads, head_dim,
                                                           (int64_t)max_pages * page_size);
   if (need && (!workspace || workspace_bytes < need)) return HSA_STEP_ERR_WORKSPACE;
   if (need && !aligned(workspace, 16)) return HSA_STEP_ERR_SHAPE;
-  const size_t cb = (size_t)n_rows * dk * ce, eb = e4m3 ? (size_t)n_rows * kv_heads : 0;
+  const size_t cb = (size_t)n_rows * row.bytes, eb = (size_t)n_rows * row.exps;
   const Range r[] = {{o, (size_t)n_seqs * d * es}, {lse, lse ? (size_t)n_seqs * heads * 4 : 0}, {workspace, need},
                      {q, span(n_seqs, q_stride, d, es)}, {k_cache, cb}, {v_cache, cb}, {k_exp, eb}, {v_exp, eb},
                      {page_table, (size_t)n_seqs * max_pages * 4}, {kv_lens, (size_t)n_seqs * 4}};
@@ -251,5 +258,162 @@ HSA_API int hsa_paged_attention(int dtype, const void* q, int64_t q_stride, int 
   a.o = o;
   a.lse = lse;
   a.ws = workspace;
-  return launch_status(hsa::launch_paged_attention(a, dtype == HSA_STEP_BF16, e4m3, head_dim, stream));
+  return launch_status(hsa::launch_paged_attention(a, dtype == HSA_STEP_BF16, row.held, head_dim, stream));
+}
+
+HSA_API int hsa_quantize_w4(int dtype, const void* w, int64_t w_stride, int64_t n_rows, int32_t d, void* codes,
+                            int8_t* exps, hipStream_t stream) {
+  const size_t es = elem_size(dtype);
+  if (!es) return HSA_STEP_ERR_DTYPE;
+  // one launch: fewer than 2^32 threads of 8 values
+  if (n_rows < 0 || n_rows > kMaxRows || d < 1 || d > kMaxStride || d % hsa::kGroup != 0 || n_rows * d >= kMaxLaunch * 8 - 2048)
+    return HSA_STEP_ERR_SHAPE;
+  if (n_rows == 0) return HSA_STEP_OK;
+  if (!w || !codes || !exps) return HSA_STEP_ERR_NULL;
+  if (!rows_ok(w, n_rows, w_stride, d, es) || !aligned(codes, 16)) return HSA_STEP_ERR_SHAPE;
+  const Range r[] = {{codes, (size_t)n_rows * d / 2}, {exps, (size_t)n_rows * d / hsa::kGroup}, {w, span(n_rows, w_stride, d, es)}};
+  if (any_overlap(r, 2)) return HSA_STEP_ERR_ALIAS;
+  return launch_status(hsa::launch_quantize_w4(w, dtype == HSA_STEP_BF16, n_rows, d, w_stride, codes, exps, stream));
+}
+
+HSA_API int hsa_linear_w4(int dtype, const void* x, int32_t n_rows, int32_t d_in, const void* w, const int8_t* w_exp,
+                          int32_t d_out, const float* row_scale, const void* residual, int32_t gelu, int out_dtype,
+                          void* y, hipStream_t stream) {
+  const size_t es = elem_size(dtype), os = elem_size(out_dtype);
+  if (!es || (out_dtype != dtype && !(dtype == HSA_STEP_BF16 && out_dtype == HSA_STEP_F32))) return HSA_STEP_ERR_DTYPE;
+  if (n_rows < 0 || d_in < 1 || d_in > kMaxStride || d_in % hsa::kGroup != 0 || d_out < 0 || d_out > kMaxStride ||
+      n_rows > kMaxStride)
+    return HSA_STEP_ERR_SHAPE;
+  if ((gelu && residual) || (out_dtype != dtype && (gelu || residual))) return HSA_STEP_ERR_SHAPE;
+  if (n_rows == 0 || d_out == 0) return HSA_STEP_OK;
+  if (!x || !w || !w_exp || !y) return HSA_STEP_ERR_NULL;
+  if (!aligned(x, 16) || !aligned(w, 16) || !aligned(y, 16) || !aligned(residual, 16) || !aligned(row_scale, 4))
+    return HSA_STEP_ERR_SHAPE;
+  const size_t yb = (size_t)n_rows * d_out * os;
+  const Range r[] = {{y, yb}, {x, (size_t)n_rows * d_in * es}, {w, (size_t)d_out * d_in / 2},
+                     {w_exp, (size_t)d_out * d_in / hsa::kGroup}, {row_scale, row_scale ? (size_t)n_rows * 4 : 0},
+                     {residual, residual && residual != y ? yb : 0}};
+  if (any_overlap(r, 1)) return HSA_STEP_ERR_ALIAS;
+  hsa::LinearW4 a{};
+  a.x = x;
+  a.w = static_cast<const uint8_t*>(w);
+  a.exps = w_exp;
+  a.rows = n_rows;
+  a.d_in = d_in;
+  a.d_out = d_out;
+  a.row_scale = row_scale;
+  a.residual = residual;
+  a.gelu = gelu != 0;
+  a.out_f32 = out_dtype != dtype;
+  a.y = y;
+  return launch_status(hsa::launch_linear_w4(a, dtype == HSA_STEP_BF16, stream));
+}
+
+HSA_API int hsa_qk_norm_rope(int dtype, const void* q, int64_t q_stride, const void* k, int64_t k_stride, int32_t n,
+                             int32_t heads, int32_t kv_heads, int32_t head_dim, const void* q_weight,
+                             const void* k_weight, float eps, const float* rope, int64_t n_pos, int32_t rope_dim,
+                             int32_t interleaved, const int32_t* pos, void* q_out, int64_t q_out_stride, void* k_out,
+                             int64_t k_out_stride, hipStream_t stream) {
+  const size_t es = elem_size(dtype);
+  if (!es) return HSA_STEP_ERR_DTYPE;
+  if (n < 0 || heads < 0 || kv_heads < 0 || (head_dim != 64 && head_dim != 128) ||
+      (int64_t)heads * head_dim > kMaxStride || (int64_t)kv_heads * head_dim > kMaxStride || !(eps > 0.f) || eps > 0x1p127f ||
+      rope_dim < 0 || rope_dim > head_dim || rope_dim % 8 != 0 || n_pos < 0 || n_pos > kMaxRows)
+    return HSA_STEP_ERR_SHAPE;
+  const int64_t d = (int64_t)heads * head_dim, dk = (int64_t)kv_heads * head_dim;
+  // one launch: fewer than 2^32 threads of 8 values
+  if ((__int128)n * (d + dk) >= kMaxLaunch * 8 - 2048) return HSA_STEP_ERR_SHAPE;
+  if (n == 0 || heads + (int64_t)kv_heads == 0) return HSA_STEP_OK;
+  if ((heads > 0 && (!q || !q_out)) || (kv_heads > 0 && (!k || !k_out)) || (rope_dim > 0 && n_pos > 0 && !rope))
+    return HSA_STEP_ERR_NULL;
+  if ((heads > 0 && (!rows_ok(q, n, q_stride, d, es) || !rows_ok(q_out, n, q_out_stride, d, es))) ||
+      (kv_heads > 0 && (!rows_ok(k, n, k_stride, dk, es) || !rows_ok(k_out, n, k_out_stride, dk, es))))
+    return HSA_STEP_ERR_SHAPE;
+  const size_t wa = es == 2 ? 16 : 4;
+  if (!aligned(q_weight, wa) || !aligned(k_weight, wa) || !aligned(rope, 16) || !aligned(pos, 4)) return HSA_STEP_ERR_SHAPE;
+  const size_t qb = heads > 0 ? span(n, q_stride, d, es) : 0, kb = kv_heads > 0 ? span(n, k_stride, dk, es) : 0;
+  const size_t qob = heads > 0 ? span(n, q_out_stride, d, es) : 0, kob = kv_heads > 0 ? span(n, k_out_stride, dk, es) : 0;
+  // queries and keys lie in one projection's output, between each other's rows: their rows may not
+  // meet, their spans may
+  auto meet = [&](const void* p, int64_t ps, int64_t pw, size_t pb, const void* o, int64_t os, int64_t ow, size_t ob) {
+    if (!overlaps(p, pb, o, ob)) return false;
+    if (ps != os) return true;
+    const int64_t row = ps * (int64_t)es;
+    int64_t at = (int64_t)(reinterpret_cast<uintptr_t>(o) - reinterpret_cast<uintptr_t>(p)) % row;
+    if (at < 0) at += row;
+    return n > 1 ? at < pw * (int64_t)es || at + ow * (int64_t)es > row : true;
+  };
+  const bool q_here = q == q_out && q_stride == q_out_stride, k_here = k == k_out && k_stride == k_out_stride;
+  if (heads > 0 && ((!q_here && meet(q, q_stride, d, qb, q_out, q_out_stride, d, qob)) ||
+                    (kv_heads > 0 && meet(k, k_stride, dk, kb, q_out, q_out_stride, d, qob))))
+    return HSA_STEP_ERR_ALIAS;
+  if (kv_heads > 0 && ((!k_here && meet(k, k_stride, dk, kb, k_out, k_out_stride, dk, kob)) ||
+                       (heads > 0 && meet(q, q_stride, d, qb, k_out, k_out_stride, dk, kob))))
+    return HSA_STEP_ERR_ALIAS;
+  if (heads > 0 && kv_heads > 0 && meet(q_out, q_out_stride, d, qob, k_out, k_out_stride, dk, kob)) return HSA_STEP_ERR_ALIAS;
+  const size_t wb = (size_t)head_dim * es, rb = rope_dim ? (size_t)n_pos * rope_dim * 4 : 0, pb = pos ? (size_t)n * 4 : 0;
+  const Range r[] = {{heads > 0 ? q_out : nullptr, qob}, {kv_heads > 0 ? k_out : nullptr, kob}, {q_weight, wb}, {k_weight, wb},
+                     {rope, rb}, {pos, pb}};
+  for (int o = 0; o < 2; ++o)
+    for (int i = 2; i < 6; ++i)
+      if (overlaps(r[o].p, r[o].n, r[i].p, r[i].n)) return HSA_STEP_ERR_ALIAS;
+  hsa::NormRope a{};
+  a.q = q;
+  a.k = k;
+  a.q_out = q_out;
+  a.k_out = k_out;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.qo_stride = q_out_stride;
+  a.ko_stride = k_out_stride;
+  a.n = n;
+  a.heads = heads;
+  a.kv_heads = kv_heads;
+  a.q_weight = q_weight;
+  a.k_weight = k_weight;
+  a.eps = eps;
+  a.rope = rope;
+  a.rope_dim = n_pos > 0 ? rope_dim : 0;
+  a.interleaved = interleaved != 0;
+  a.n_pos = n_pos;
+  a.pos = pos;
+  return launch_status(hsa::launch_norm_rope(a, dtype == HSA_STEP_BF16, head_dim, stream));
+}
+
+HSA_API int hsa_page_plan(const int32_t* past, const int32_t* fresh, int32_t n_seqs, int32_t page_size, int32_t max_pages,
+                          int32_t* page_table, const int32_t* free_pages, int32_t n_free, const int32_t* free_at,
+                          int32_t n_tokens, int32_t* cu, int32_t* kv_lens, int32_t* pos, int32_t* slots,
+                          int32_t* free_next, hipStream_t stream) {
+  if (n_seqs < 0 || n_seqs == INT32_MAX || page_size < 1 || max_pages < 0 || (int64_t)max_pages * page_size > kMaxKeys || n_free < 0 ||
+      n_free > kMaxKeys || n_tokens < 0 || n_tokens >= kMaxKeys || !fits(n_seqs, max_pages, 4))
+    return HSA_STEP_ERR_SHAPE;
+  if ((n_seqs > 0 && (!past || !fresh || !kv_lens || (max_pages > 0 && !page_table))) || (n_free > 0 && !free_pages) ||
+      !free_at || !free_next || !cu || (n_tokens > 0 && (!pos || !slots)))
+    return HSA_STEP_ERR_NULL;
+  const void* ints[] = {past, fresh, page_table, free_pages, free_at, cu, kv_lens, pos, slots, free_next};
+  for (const void* p : ints)
+    if (!aligned(p, 4)) return HSA_STEP_ERR_SHAPE;
+  const size_t sb = (size_t)n_seqs * 4, tb = (size_t)n_tokens * 4;
+  // kv_lens may be past, free_next free_at: a step that goes on from the last one's
+  const Range r[] = {{page_table, (size_t)n_seqs * max_pages * 4}, {cu, sb + 4}, {kv_lens, sb}, {pos, tb}, {slots, tb}, {free_next, 12},
+                     {kv_lens == past ? nullptr : past, sb}, {fresh, sb}, {free_pages, (size_t)n_free * 4},
+                     {free_at == free_next ? nullptr : free_at, 12}};
+  if (any_overlap(r, 6)) return HSA_STEP_ERR_ALIAS;
+  hsa::PagePlan a{};
+  a.past = past;
+  a.fresh = fresh;
+  a.n_seqs = n_seqs;
+  a.page_size = page_size;
+  a.max_pages = max_pages;
+  a.page_table = page_table;
+  a.free_pages = free_pages;
+  a.n_free = n_free;
+  a.free_at = free_at;
+  a.n_tokens = n_tokens;
+  a.cu = cu;
+  a.kv_lens = kv_lens;
+  a.pos = pos;
+  a.slots = slots;
+  a.free_next = free_next;
+  return launch_status(hsa::launch_page_plan(a, stream));
 }

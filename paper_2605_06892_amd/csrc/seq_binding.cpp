@@ -1,5 +1,5 @@
 // Python binding of the calls over several sequences (hsa_cache_store ..
-// hsa_paged_attention), whose kernels take 3 us for a small batch: what they
+// hsa_page_plan), whose kernels take 3 us for a small batch: what they
 // check of their tensors costs 3.5 us in Python and 0.2 us here. Checks of layout, types
 // and shapes, then the C entry point, whose status is returned; no computation.
 //
@@ -112,7 +112,12 @@ int64_t row_stride(const at::Tensor& t) { return t.size(0) > 1 ? t.stride(0) : t
 const int8_t* bytes(const at::Tensor* t) { return t ? static_cast<const int8_t*>(t->data_ptr()) : nullptr; }
 const int32_t* ints(const at::Tensor& t) { return static_cast<const int32_t*>(t.data_ptr()); }
 
-// Caches of rows' dtype, or of codes with their exponents; their dtype code.
+void exponents(const Here& here, const at::Tensor* e, int64_t n, int64_t width, const char* what) {
+  here.held(e);
+  if (!e || e->scalar_type() != at::kChar || e->dim() != 2 || e->size(0) != n || e->size(1) != width) type_error(what);
+}
+
+// Caches of rows' dtype, or of codes with their exponents; their dtype code. `width` in values.
 struct Caches {
   const at::Tensor &k, &v;
   const at::Tensor *k_exp, *v_exp;
@@ -126,18 +131,21 @@ Caches caches(const Here& here, const at::Tensor& rows, const at::Tensor& k, con
   if (k.scalar_type() != v.scalar_type() || k.dim() != 2 || k.sizes() != v.sizes())
     type_error("k_cache and v_cache must match: [n_rows, kv_heads * head_dim]");
   Caches c{k, v, nullptr, nullptr, HSA_STEP_E4M3, k.size(0), k.size(1)};
-  if (k.scalar_type() != at::kFloat8_e4m3fn) {
-    if (k.scalar_type() != rows.scalar_type()) type_error("caches hold the rows' dtype or float8_e4m3fn");
+  if (k.scalar_type() == at::kByte) {
+    c.dtype = HSA_STEP_E2M1;
+    c.width *= 2;
+    exponents(here, ke, c.n_rows, c.width / 32, "uint8 caches (e2m1) need int8 exponents [n_rows, kv_heads * head_dim / 32]");
+    exponents(here, ve, c.n_rows, c.width / 32, "uint8 caches (e2m1) need int8 exponents [n_rows, kv_heads * head_dim / 32]");
+  } else if (k.scalar_type() != at::kFloat8_e4m3fn) {
+    if (k.scalar_type() != rows.scalar_type()) type_error("caches hold the rows' dtype, float8_e4m3fn, or uint8 (e2m1)");
     c.dtype = dtype_of(rows);
+    return c;
   } else {
-    for (const at::Tensor* e : {ke, ve}) {
-      here.held(e);
-      if (!e || e->scalar_type() != at::kChar || e->dim() != 2 || e->size(0) != c.n_rows || e->size(1) != kv_heads)
-        type_error("float8_e4m3fn caches need int8 exponents [n_rows, kv_heads]");
-    }
-    c.k_exp = ke;
-    c.v_exp = ve;
+    exponents(here, ke, c.n_rows, kv_heads, "float8_e4m3fn caches need int8 exponents [n_rows, kv_heads]");
+    exponents(here, ve, c.n_rows, kv_heads, "float8_e4m3fn caches need int8 exponents [n_rows, kv_heads]");
   }
+  c.k_exp = ke;
+  c.v_exp = ve;
   return c;
 }
 
@@ -257,6 +265,129 @@ int paged(Args& a) {
                              ws ? ws->data_ptr() : nullptr, ws ? ws->numel() * ws->element_size() : 0, stream);
 }
 
+// fp32 values that may be missing
+const float* floats(const Here& here, const at::Tensor* t) {
+  if (!t) return nullptr;
+  here.held(*t);
+  if (t->scalar_type() != at::kFloat) type_error("scales and rotations are fp32");
+  return static_cast<const float*>(t->data_ptr());
+}
+void* data(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+
+// (device, stream, w, codes, exps)
+int quantize(Args& a) {
+  const Here here{a.integer()};
+  const hipStream_t stream = static_cast<hipStream_t>(a.handle());
+  const at::Tensor &w = a.tensor(), &codes = a.tensor(), &exps = a.tensor();
+  here.rows(w);
+  here.held(codes);
+  const int dt = dtype_of(w);
+  const int64_t n = w.size(0), d = w.size(1);
+  if (codes.scalar_type() != at::kByte) type_error("codes are uint8");
+  if (d > INT32_MAX || d % 32 || codes.dim() != 2 || codes.size(0) != n || codes.size(1) * 2 != d)
+    value_error("w is [n_rows, d] with d a multiple of 32, codes [n_rows, d / 2]");
+  exponents(here, &exps, n, d / 32, "exponents are int8 [n_rows, d / 32]");
+  const Unlocked unlocked;
+  return hsa_quantize_w4(dt, w.data_ptr(), row_stride(w), n, (int32_t)d, codes.data_ptr(),
+                         static_cast<int8_t*>(exps.data_ptr()), stream);
+}
+
+// (device, stream, x, n_rows, w, w_exp, y, residual, row_scale, gelu)
+int linear(Args& a) {
+  const Here here{a.integer()};
+  const hipStream_t stream = static_cast<hipStream_t>(a.handle());
+  const at::Tensor& x = a.tensor();
+  const int32_t n = a.int32();
+  const at::Tensor &w = a.tensor(), &we = a.tensor(), &y = a.tensor();
+  const at::Tensor *residual = a.tensor_or_none(), *scale = a.tensor_or_none();
+  const int gelu = PyObject_IsTrue(a.next());
+  if (gelu < 0) throw std::exception();
+  for (const at::Tensor* t : {&x, &w, &y, residual}) here.held(t);
+  const int dt = dtype_of(x), out = dtype_of(y);
+  if (residual) same_type(*residual, y);
+  if (w.scalar_type() != at::kByte) type_error("weights are uint8 codes");
+  if (x.dim() != 2 || w.dim() != 2 || y.dim() != 2 || n > x.size(0) || n > y.size(0) || w.size(1) * 2 != x.size(1) ||
+      y.size(1) != w.size(0) || x.size(1) > INT32_MAX || w.size(0) > INT32_MAX ||
+      (residual && (residual->dim() != 2 || n > residual->size(0) || residual->size(1) != y.size(1))) ||
+      (scale && n > scale->numel()))
+    value_error("x is [n_rows, d_in], w [d_out, d_in / 2], y and residual [n_rows, d_out], row_scale [n_rows]");
+  exponents(here, &we, w.size(0), x.size(1) / 32, "weights need int8 exponents [d_out, d_in / 32]");
+  const float* s = floats(here, scale);
+  const Unlocked unlocked;
+  return hsa_linear_w4(dt, x.data_ptr(), n, (int32_t)x.size(1), w.data_ptr(), bytes(&we), (int32_t)w.size(0), s, data(residual),
+                       gelu, out, y.data_ptr(), stream);
+}
+
+// (device, stream, q, k, heads, kv_heads, head_dim, q_out, k_out, q_weight,
+//  k_weight, eps, rope, pos, interleaved)
+int norm_rope(Args& a) {
+  const Here here{a.integer()};
+  const hipStream_t stream = static_cast<hipStream_t>(a.handle());
+  const at::Tensor *q = a.tensor_or_none(), *k = a.tensor_or_none();
+  const int32_t heads = a.int32(), kv_heads = a.int32(), head_dim = a.int32();
+  const at::Tensor *qo = a.tensor_or_none(), *ko = a.tensor_or_none(), *qw = a.tensor_or_none(), *kw = a.tensor_or_none();
+  const float eps = (float)a.real();
+  const at::Tensor *rope = a.tensor_or_none(), *pos = a.tensor_or_none();
+  const int interleaved = PyObject_IsTrue(a.next());
+  if (interleaved < 0) throw std::exception();
+  if (!q && !k) type_error("expected queries, keys or both");
+  if (!q != !qo || !k != !ko || !q != (heads == 0) || !k != (kv_heads == 0))
+    value_error("queries and keys come with their outputs and their number of heads, or none of these");
+  const at::Tensor& one = q ? *q : *k;
+  const int dt = dtype_of(one);
+  for (const at::Tensor* t : {q, k, qo, ko}) {
+    if (!t) continue;
+    here.rows(*t);
+    same_type(one, *t);
+    if (t->size(0) != one.size(0) || t->size(1) != (int64_t)(t == q || t == qo ? heads : kv_heads) * head_dim)
+      value_error("queries are [n, heads * head_dim], keys [n, kv_heads * head_dim], their outputs the same");
+  }
+  if (one.size(0) > INT32_MAX) value_error("a size does not fit 32 bits");
+  for (const at::Tensor* t : {qw, kw}) {
+    if (!t) continue;
+    here.held(*t);
+    same_type(one, *t);
+    if (t->numel() != head_dim) value_error("norm weights have head_dim values");
+  }
+  const float* table = floats(here, rope);
+  if (rope && (rope->dim() != 3 || rope->size(2) != 2 || rope->size(1) > INT32_MAX / 2))
+    value_error("rope is [positions, rope_dim / 2, 2]");
+  if (pos) {
+    here.int32s(*pos);
+    if (pos->numel() != one.size(0)) value_error("pos has one position per row");
+  }
+  const Unlocked unlocked;
+  return hsa_qk_norm_rope(dt, data(q), q ? row_stride(*q) : 0, data(k), k ? row_stride(*k) : 0, (int32_t)one.size(0), heads,
+                          kv_heads, head_dim, data(qw), data(kw), eps, table, rope ? rope->size(0) : 0,
+                          rope ? (int32_t)rope->size(1) * 2 : 0, interleaved, pos ? ints(*pos) : nullptr, data(qo),
+                          qo ? row_stride(*qo) : 0, data(ko), ko ? row_stride(*ko) : 0, stream);
+}
+
+// (device, stream, past, fresh, page_size, page_table, free_pages, free_at, cu,
+//  kv_lens, pos, slots, free_next)
+int plan(Args& a) {
+  const Here here{a.integer()};
+  const hipStream_t stream = static_cast<hipStream_t>(a.handle());
+  const at::Tensor &past = a.tensor(), &fresh = a.tensor();
+  const int32_t page_size = a.int32();
+  const at::Tensor &table = a.tensor(), &free_pages = a.tensor(), &free_at = a.tensor(), &cu = a.tensor(),
+                   &kv_lens = a.tensor(), &pos = a.tensor(), &slots = a.tensor(), &free_next = a.tensor();
+  for (const at::Tensor* t : {&past, &fresh, &table, &free_pages, &free_at, &cu, &kv_lens, &pos, &slots, &free_next})
+    here.int32s(*t);
+  const int64_t n = past.numel();
+  if (n > INT32_MAX || fresh.numel() != n || kv_lens.numel() != n || cu.numel() != n + 1 || table.dim() != 2 || table.size(0) != n ||
+      table.size(1) > INT32_MAX || free_pages.numel() > INT32_MAX || free_at.numel() != 3 || free_next.numel() != 3 ||
+      pos.numel() != slots.numel() || pos.numel() > INT32_MAX)
+    value_error("past, fresh and kv_lens are [n_seqs], cu [n_seqs + 1], page_table [n_seqs, max_pages], pos and slots "
+                "[n_tokens], free_at and free_next [3]");
+  const Unlocked unlocked;
+  return hsa_page_plan(ints(past), ints(fresh), (int32_t)n, page_size, (int32_t)table.size(1),
+                       static_cast<int32_t*>(table.data_ptr()), ints(free_pages), (int32_t)free_pages.numel(), ints(free_at),
+                       (int32_t)pos.numel(), static_cast<int32_t*>(cu.data_ptr()), static_cast<int32_t*>(kv_lens.data_ptr()),
+                       static_cast<int32_t*>(pos.data_ptr()), static_cast<int32_t*>(slots.data_ptr()),
+                       static_cast<int32_t*>(free_next.data_ptr()), stream);
+}
+
 template <class F>
 PyObject* call(PyObject* const* at, Py_ssize_t n, F f) {
   try {
@@ -281,6 +412,10 @@ PyObject* cache_load(PyObject*, PyObject* const* at, Py_ssize_t n) {
 }
 PyObject* packed_attention(PyObject*, PyObject* const* at, Py_ssize_t n) { return call(at, n, packed); }
 PyObject* paged_attention(PyObject*, PyObject* const* at, Py_ssize_t n) { return call(at, n, paged); }
+PyObject* quantize_w4(PyObject*, PyObject* const* at, Py_ssize_t n) { return call(at, n, quantize); }
+PyObject* linear_w4(PyObject*, PyObject* const* at, Py_ssize_t n) { return call(at, n, linear); }
+PyObject* qk_norm_rope(PyObject*, PyObject* const* at, Py_ssize_t n) { return call(at, n, norm_rope); }
+PyObject* page_plan(PyObject*, PyObject* const* at, Py_ssize_t n) { return call(at, n, plan); }
 
 PyCFunction fast(PyObject* (*f)(PyObject*, PyObject* const*, Py_ssize_t)) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f));
@@ -289,6 +424,10 @@ PyMethodDef methods[] = {{"cache_store", fast(cache_store), METH_FASTCALL, nullp
                          {"cache_load", fast(cache_load), METH_FASTCALL, nullptr},
                          {"packed_attention", fast(packed_attention), METH_FASTCALL, nullptr},
                          {"paged_attention", fast(paged_attention), METH_FASTCALL, nullptr},
+                         {"quantize_w4", fast(quantize_w4), METH_FASTCALL, nullptr},
+                         {"linear_w4", fast(linear_w4), METH_FASTCALL, nullptr},
+                         {"qk_norm_rope", fast(qk_norm_rope), METH_FASTCALL, nullptr},
+                         {"page_plan", fast(page_plan), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_seq_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -1,4 +1,4 @@
-// What the kernels over several sequences share: e4m3 rows, divisions by
+// What the kernels over several sequences share: e4m3 and e2m1 rows, divisions by
 // sizes known on the host, and the launch arguments of their entry points.
 #pragma once
 
@@ -9,6 +9,17 @@ namespace hsa {
 // Exponents of e4m3 cache rows. 2^e and 2^-e are normal numbers, the least code
 // (2^-9) times 2^kExpMin still is one, and 448 * 2^kExpMax is finite.
 constexpr int kExpMin = -117, kExpMax = 119;
+
+// How rows are held: in their own type; e4m3 codes with an exponent per row and head;
+// e2m1 codes, two to a byte, with an exponent per group of 32 values.
+enum Held { kOwn, kE4M3, kE2M1 };
+constexpr int kGroup = 32;
+
+// Exponents of e2m1 groups. 2^e and 2^-e are normal numbers, so is the least code (1/2) times
+// 2^kExp4Min, and 6 * 2^kExp4Max is finite. kExp4Nan marks a group that holds a
+// value which is not finite: as the scale operand of the conversions from e2m1, 2^kExp4Nan (all
+// exponent bits set) makes every code, 0 too, a NaN.
+constexpr int kExp4Min = -125, kExp4Max = 125, kExp4Nan = -128;
 
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
@@ -25,13 +36,14 @@ struct FastDiv {
   __device__ __forceinline__ uint32_t quot(uint32_t x) const { return (__umulhi(x, m) + x) >> s; }
 };
 
-// Fresh rows in, or out of, a cache (cache.hip). `dtype` is the rows' type;
-// e4m3: the cache holds codes and exponents, else rows of dtype.
+// Fresh rows in, or out of, a cache (cache.hip): rows of bf16 or fp32 values, and how the
+// cache holds them.
 struct CacheRows {
-  bool bf16, e4m3;
+  bool bf16;
+  Held held;
   const void *src_k, *src_v;    // rows read
   void *dst_k, *dst_v;          // rows written
-  int8_t *k_exp, *v_exp;        // e4m3
+  int8_t *k_exp, *v_exp;        // of codes
   long k_stride, v_stride;      // of the compact rows, in elements
   const int32_t* idx;
   int n;
@@ -40,6 +52,9 @@ struct CacheRows {
 };
 hipError_t launch_cache_store(const CacheRows& c, hipStream_t s);
 hipError_t launch_cache_load(const CacheRows& c, hipStream_t s);
+// Rows of weights into e2m1 groups (cache.hip): d % 32 == 0, rows `stride` elements apart.
+hipError_t launch_quantize_w4(const void* w, bool bf16, long n, int d, long stride, void* codes, int8_t* exps,
+                              hipStream_t s);
 
 // Attention of packed sequences (packed_attention.hip). Strides in elements.
 struct PackedArgs {
@@ -73,6 +88,48 @@ struct PagedArgs {
 };
 // Workspace bytes of a launch, 0 where no sequence can be split.
 size_t paged_attention_bytes(int n_seqs, int kv_heads, int group, int head_dim, long max_len);
-hipError_t launch_paged_attention(const PagedArgs& a, bool bf16, bool e4m3, int head_dim, hipStream_t s);
+hipError_t launch_paged_attention(const PagedArgs& a, bool bf16, Held held, int head_dim, hipStream_t s);
+
+// Rows times weights in e2m1 groups (linear_w4.hip):
+// y[m][o] = act(row_scale[m] sum_k x[m][k] w[o][k]) + residual[m][o].
+struct LinearW4 {
+  const void* x;          // [rows, d_in]
+  const uint8_t* w;       // [d_out, d_in / 2]
+  const int8_t* exps;     // [d_out, d_in / 32]
+  int rows, d_in, d_out;
+  const float* row_scale;
+  const void* residual;   // of the output's type
+  int gelu, out_f32;      // out_f32: bf16 rows, fp32 output
+  void* y;
+};
+hipError_t launch_linear_w4(const LinearW4& a, bool bf16, hipStream_t s);
+
+// Norms of query and key heads and their rotation (norm_rope.hip). Strides in elements.
+struct NormRope {
+  const void *q, *k;
+  void *q_out, *k_out;
+  long q_stride, k_stride, qo_stride, ko_stride;
+  int n, heads, kv_heads;
+  const void *q_weight, *k_weight;
+  float eps;
+  const float* rope;  // [n_pos, rope_dim / 2] (cos, sin)
+  int rope_dim, interleaved;
+  int64_t n_pos;
+  const int32_t* pos;
+};
+hipError_t launch_norm_rope(const NormRope& a, bool bf16, int head_dim, hipStream_t s);
+
+// Pages and cache rows of fresh tokens (page_plan.hip).
+struct PagePlan {
+  const int32_t *past, *fresh;
+  int n_seqs, page_size, max_pages;
+  int32_t* page_table;
+  const int32_t* free_pages;
+  int n_free;
+  const int32_t* free_at;
+  int n_tokens;
+  int32_t *cu, *kv_lens, *pos, *slots, *free_next;
+};
+hipError_t launch_page_plan(const PagePlan& a, hipStream_t s);
 
 }  // namespace hsa

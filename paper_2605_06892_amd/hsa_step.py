@@ -20,6 +20,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhsa_ste
 F32 = 0
 BF16 = 1
 E4M3 = 2  # 8-bit cache rows
+E2M1 = 4  # 4-bit cache rows
 
 _STATUS = {
     0: "HSA_STEP_OK",
@@ -85,6 +86,11 @@ def lib() -> ctypes.CDLL:
             "hsa_paged_attention_workspace_bytes": (S, [ctypes.c_int, I32, I32, I32, I32, I64]),
             "hsa_paged_attention": (ctypes.c_int, [ctypes.c_int, P, I64, ctypes.c_int, P, P, P, P, P, I32, P, I32, I32,
                                                    I32, I32, I32, I32, F, P, P, P, S, P]),
+            "hsa_quantize_w4": (ctypes.c_int, [ctypes.c_int, P, I64, I64, I32, P, P, P]),
+            "hsa_linear_w4": (ctypes.c_int, [ctypes.c_int, P, I32, I32, P, P, I32, P, P, I32, ctypes.c_int, P, P]),
+            "hsa_qk_norm_rope": (ctypes.c_int, [ctypes.c_int, P, I64, P, I64, I32, I32, I32, I32, P, P, F, P, I64, I32, I32, P,
+                                                P, I64, P, I64, P]),
+            "hsa_page_plan": (ctypes.c_int, [P, P, I32, I32, I32, P, P, I32, P, I32, P, P, P, P, P, P]),
             "hsa_stack_iteration": (ctypes.c_int, [ctypes.POINTER(HsaStack), I32, I32, I32, I32, F, F, P, P,
                                                    I32, I32, P, P, P]),
         }
@@ -126,6 +132,10 @@ EXPORTED = (
     "hsa_packed_attention",
     "hsa_paged_attention_workspace_bytes",
     "hsa_paged_attention",
+    "hsa_quantize_w4",
+    "hsa_linear_w4",
+    "hsa_qk_norm_rope",
+    "hsa_page_plan",
     "hsa_stack_iteration",
 )
 
@@ -468,8 +478,9 @@ def _stream_here(stream, dev: int):
 
 def hsa_cache_store(k, v, idx, n: int, kv_heads: int, k_cache, v_cache, k_exp=None, v_exp=None, stream=None) -> None:
     """k_cache[idx[:n]] = k[:n] and the same for v, quantized on the way into
-    float8_e4m3fn caches (k_exp, v_exp: their int8 exponents [n_rows, kv_heads]);
-    an index outside the cache skips its row."""
+    float8_e4m3fn caches (k_exp, v_exp: their int8 exponents [n_rows, kv_heads]) or
+    uint8 ones of e2m1 codes [n_rows, kv_heads * head_dim / 2] (exponents [n_rows,
+    kv_heads * head_dim / 32]); an index outside the cache skips its row."""
     dev = _here()
     st = (_seq or _binding()).cache_store(dev, _stream_here(stream, dev), k, v, idx, n, kv_heads, k_cache, v_cache, k_exp,
                                           v_exp)
@@ -518,6 +529,51 @@ def hsa_paged_attention(q, k_cache, v_cache, page_table, kv_lens, page_size: int
                                               page_size, heads, kv_heads, head_dim, scale, o, workspace, k_exp, v_exp, lse)
     if st:
         raise HsaStepError("hsa_paged_attention", st)
+
+
+def hsa_quantize_w4(w, codes, exps, stream=None) -> None:
+    """Rows of weights [n_rows, d] into e2m1 codes, uint8 [n_rows, d / 2], and the int8
+    exponents of their groups of 32 [n_rows, d / 32]."""
+    dev = _here()
+    st = (_seq or _binding()).quantize_w4(dev, _stream_here(stream, dev), w, codes, exps)
+    if st:
+        raise HsaStepError("hsa_quantize_w4", st)
+
+
+def hsa_linear_w4(x, n_rows: int, w, w_exp, y, residual=None, row_scale=None, gelu: bool = False, stream=None) -> None:
+    """hsa_linear with weights from hsa_quantize_w4, for a few rows: y[:n_rows] =
+    act(row_scale * (x W^T)) (+ residual). y is of x's dtype, or fp32."""
+    dev = _here()
+    st = (_seq or _binding()).linear_w4(dev, _stream_here(stream, dev), x, n_rows, w, w_exp, y, residual, row_scale, gelu)
+    if st:
+        raise HsaStepError("hsa_linear_w4", st)
+
+
+def hsa_qk_norm_rope(q, k, heads: int, kv_heads: int, head_dim: int, q_out, k_out, q_weight=None, k_weight=None,
+                     eps: float = RMS_EPS, rope=None, pos=None, interleaved: bool = False, stream=None) -> None:
+    """RMS norms of every head of q and k, and their rotation by the rows pos (None: the
+    row's own index) of rope, fp32 (cos, sin) pairs [positions, rope_dim / 2, 2] (None:
+    none); a position outside it leaves its row unturned. The outputs may be q and k
+    themselves; q or k may be None with 0 heads."""
+    dev = _here()
+    st = (_seq or _binding()).qk_norm_rope(dev, _stream_here(stream, dev), q, k, heads, kv_heads, head_dim, q_out, k_out,
+                                           q_weight, k_weight, eps, rope, pos, interleaved)
+    if st:
+        raise HsaStepError("hsa_qk_norm_rope", st)
+
+
+def hsa_page_plan(past, fresh, page_size: int, page_table, free_pages, free_at, cu, kv_lens, pos, slots, free_next,
+                  stream=None) -> None:
+    """Pages (page_table, from the ring free_pages), offsets (cu), lengths (kv_lens),
+    positions and cache rows (pos, slots; -1 behind the last) of fresh[s] tokens for each
+    sequence with past[s] rows. free_at, free_next: int32 [3], the ring's first free
+    entry, the number of free ones, and the pages that were lacking. kv_lens may be past
+    and free_next free_at. All int32."""
+    dev = _here()
+    st = (_seq or _binding()).page_plan(dev, _stream_here(stream, dev), past, fresh, page_size, page_table, free_pages,
+                                        free_at, cu, kv_lens, pos, slots, free_next)
+    if st:
+        raise HsaStepError("hsa_page_plan", st)
 
 
 def make_stack(*, x, v_hat, budget, w_embed, w_head, layers, caches, idx, n_active, xa, h, q, o, v_fresh,
