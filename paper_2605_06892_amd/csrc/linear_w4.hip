@@ -1,104 +1,207 @@
 // Rows times weights in e2m1 groups: y = act(s (x W^T)) + r for a few rows, bound by reading W.
 //
-// A wave takes 16 outputs (the rows of the matrix instructions' tile) and 128 inputs of W at a
-// time: each lane loads 16 bytes, the 32 codes of one group, and that group's exponent, which
-// the conversion to bf16 takes as its operand: exact, one instruction for two weights, and no
-// scaling of sums. Slot lane / 16 of the contraction holds that group, 8 values to an instruction, so
-// x is read in the same order. The rows of x are the tile's columns, 16 to a tile.
-// The waves of a workgroup take 128 inputs each in turn and are joined in LDS.
+// A wave takes 16 outputs (the rows of the matrix instructions' tile) and units of 512 inputs. In each of
+// a unit's four steps a lane loads 16 bytes, the 32 codes of one group, 64 bytes of one row for its four
+// lanes; the exponents of all four are one load before them (a byte of its own for every step, of 16 rows each, took a
+// quarter of the time). The conversion to bf16 takes the exponent as its operand: exact, one
+// instruction for two weights, and no scaling of sums. Slot lane / 16 of the contraction holds that group, 8 values to an
+// instruction; x is read from LDS in the same order. The rows of x are the tile's columns.
+// Codes are loaded a unit ahead of the products, each step's into the registers that its products have
+// freed; the waves of a workgroup that share inputs (`outs` of them) load x together, those that share
+// outputs (`splits`) take units in turn and are joined in LDS.
+//
+// fp32 rows are taken as three bf16 parts, cut from the top: 8 + 8 + 8 bits are all that fp32 has, so every
+// product is exact here too, and sums are in fp32 as before (what of a value lies under 2^-133, bf16's least, is
+// left out). The parts are columns of their own, five rows to a tile, summed at the end. The fp32
+// matrix instructions are 16 times slower than the bf16 ones: 5 rows of 8960 by 1537 outputs take 16 us with them,
+// 12 so, of 8192 by 16384 48 and 21.
+//
+// One row of 8192 by 32768 outputs: 30 us, 4.7 TB/s; 16 rows 37 us.
 #include "seq_common.h"
+
+#include <algorithm>
+#include <type_traits>
 
 namespace hsa {
 namespace {
 
-constexpr int kOuts = 16;   // outputs of a tile, and rows of x of one
-constexpr int kStep = 128;  // inputs of a wave's load
-constexpr int kWaves = 8;
+constexpr int kOuts = 16;   // outputs of a tile, and columns for rows of x
+constexpr int kUnit = 512;  // inputs of a unit: 16 groups, four steps
+constexpr int kUnitGroups = kUnit / kGroup;
+constexpr int kMostWaves = 8;
 
 __device__ __forceinline__ float gelu_exact(float x) {
   const float y = 0.7978845608028654f * fmaf(0.044715f * x, x * x, x);
   return x / (1.f + expf(-2.f * y));
 }
 
-// 8 codes of a word as bf16, times 2^e in `scale`
+// 8 codes of a word as bf16, times a power of two
 __device__ __forceinline__ bf16x8 widen8(unsigned c, float scale) {
   const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1);
   const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2), t = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3);
   return (bf16x8){p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
 }
 
-template <bool BF16, int NT>
-__global__ __launch_bounds__(kWaves * kWave) void linear_w4_kernel(LinearW4 a) {
-  __shared__ __attribute__((aligned(16))) f32x4 parts[kWaves][NT][kWave];
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const int l16 = lane & 15, grp = lane >> 4;
-  const int o0 = blockIdx.x * kOuts, m0 = blockIdx.y * (kOuts * NT);
-  const long w_row = min(o0 + l16, a.d_out - 1);
-  const uint8_t* w = a.w + w_row * (a.d_in / 2);
-  const int8_t* e = a.exps + w_row * (a.d_in / kGroup);
-  long x_row[NT];
+// The three bf16 parts of 8 fp32 values. What is not finite is its first part alone.
+__device__ __forceinline__ void cut(const u32x4 (&x)[2], u32x4 (&part)[3]) {
+  unsigned h[8], m[8], l[8];
 #pragma unroll
-  for (int t = 0; t < NT; ++t) x_row[t] = (long)min(m0 + t * kOuts + l16, a.rows - 1) * a.d_in;
+  for (int j = 0; j < 8; ++j) {
+    const unsigned u = x[j >> 2][j & 3], mag = u & 0x7fffffffu;
+    h[j] = (u & 0xffff0000u) | (mag > 0x7f800000u ? 0x00400000u : 0u);
+    const float r = mag < 0x7f800000u ? __uint_as_float(u) - __uint_as_float(h[j]) : 0.f;
+    m[j] = __float_as_uint(r);
+    l[j] = __float_as_uint(r - __uint_as_float(m[j] & 0xffff0000u));
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {  // the upper halves of two
+    part[0][j] = __builtin_amdgcn_perm(h[2 * j + 1], h[2 * j], 0x07060302);
+    part[1][j] = __builtin_amdgcn_perm(m[2 * j + 1], m[2 * j], 0x07060302);
+    part[2][j] = __builtin_amdgcn_perm(l[2 * j + 1], l[2 * j], 0x07060302);
+  }
+}
 
+// Workgroups of splits * outs waves; NT tiles of rows of x; XS rows of x loaded by each wave of a split.
+template <bool BF16, int NT, int XS>
+__global__ __launch_bounds__(kMostWaves * kWave) void linear_w4_kernel(LinearW4 a, int outs, int splits) {
+  constexpr int PARTS = BF16 ? 1 : 3;           // rows in LDS of a row of x
+  constexpr int ROWS = NT * (BF16 ? kOuts : 5); // rows of x of a workgroup
+  constexpr int XL = BF16 ? 1 : 2;              // loads of 16 bytes for 8 values
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int ks = wave / outs, no = wave - ks * outs;
+  const int l16 = lane & 15, grp = lane >> 4;
+  const int o0 = blockIdx.x * (kOuts * outs), m0 = blockIdx.y * ROWS;
+  const int rows = min(a.rows - m0, ROWS), x_rows = XS * outs * PARTS;
+  const int groups = a.d_in / kGroup, units = (groups + kUnitGroups - 1) / kUnitGroups;
+  // outputs past the last repeat it and are not stored
+  const long w_row = min(o0 + no * kOuts + l16, a.d_out - 1);
+  const uint8_t* w = a.w + w_row * (a.d_in / 2);
+  const int8_t* exps = a.exps + w_row * groups;
+
+  // x of a unit in LDS, two units of each split: row r at r * 1 KB, its 16-byte chunk c at c ^ (r & 7), so that
+  // 8 rows' reads of one chunk spread over the banks. Rows past the last repeat it.
+  char* xl = lds + ks * 2 * x_rows * 1024;
+  u32x4 xr[XS][XL];
+  auto load_x = [&](int u) {
+    const int k = min(u * kUnit + lane * 8, a.d_in - 8);
+#pragma unroll
+    for (int i = 0; i < XS; ++i) {
+      const char* p = static_cast<const char*>(a.x) + ((long)(m0 + min(i * outs + no, rows - 1)) * a.d_in + k) * (BF16 ? 2 : 4);
+#pragma unroll
+      for (int j = 0; j < XL; ++j) xr[i][j] = *reinterpret_cast<const u32x4*>(p + j * 16);
+    }
+  };
+  auto stage = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < XS; ++i) {
+      u32x4 part[PARTS];
+      if constexpr (BF16) part[0] = xr[i][0];
+      else cut(xr[i], part);
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) {
+        const int r = (i * outs + no) * PARTS + p;
+        *reinterpret_cast<u32x4*>(xl + (buf * x_rows + r) * 1024 + (lane ^ (r & 7)) * 16) = part[p];
+      }
+    }
+  };
+  int x_row[NT];  // of this lane's column
+#pragma unroll
+  for (int t = 0; t < NT; ++t) x_row[t] = min(t * (BF16 ? kOuts : 15) + l16, rows * PARTS - 1);
+
+  u32x4 c[4], e, e_next;  // codes of the steps; exponents, a word for each step
   f32x4 acc[NT];
 #pragma unroll
   for (int t = 0; t < NT; ++t) acc[t] = (f32x4){};
-  for (int k0 = wave * kStep; k0 < a.d_in; k0 += kWaves * kStep) {
-    const int k = k0 + grp * kGroup;
-    const bool in = k < a.d_in;  // the last step may have fewer groups: 0 times 0
-    u32x4 c = {};
-    float s = 1.f;
-    if (in) {
-      c = *reinterpret_cast<const u32x4*>(w + k / 2);
-      s = pow2(e[k / kGroup]);
-    }
-    if constexpr (BF16) {
-      bf16x8 x[NT][4];
+  auto load_c = [&](int u, int i) {  // of a whole unit
+    c[i] = *reinterpret_cast<const u32x4*>(w + (long)(u * kUnitGroups + i * 4 + grp) * 16);
+  };
+  auto multiply = [&](int i, int buf, bool gone) {
+    bf16x8 x[NT][4];
 #pragma unroll
-      for (int t = 0; t < NT; ++t)
+    for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[t][i] = (bf16x8){};
-          if (in) x[t][i] = *reinterpret_cast<const bf16x8*>(static_cast<const bf16*>(a.x) + x_row[t] + k + i * 8);
-        }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bf16x8 y = widen8(c[i], s);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, x[t][i], acc[t], 0, 0, 0);
+      for (int j = 0; j < 4; ++j) {
+        x[t][j] = *reinterpret_cast<const bf16x8*>(xl + (buf * x_rows + x_row[t]) * 1024 + ((i * 16 + grp * 4 + j) ^ (x_row[t] & 7)) * 16);
+        if (gone) x[t][j] = (bf16x8){};
       }
-    } else {
+    const float s = pow2((int8_t)(e[i] >> (8 * grp)));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f32x4 x[NT][2];
+    for (int j = 0; j < 4; ++j) {
+      const bf16x8 y = widen8(c[i][j], s);
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+      for (int t = 0; t < NT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, x[t][j], acc[t], 0, 0, 0);
+    }
+  };
+  auto meet = [&] {
+    if (outs > 1) __syncthreads();
+    else __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");
+  };
+  // whole units, as many in every split
+  const int turns = a.d_in / kUnit / splits;
+  int buf = 0;
+  auto unit = [&](int u, auto more) {
+    meet();  // this unit's x is in LDS, and the last one's has been read
+    if constexpr (more) {
+      __builtin_memcpy(&e_next, exps + (u + splits) * kUnitGroups, 16);
+      load_x(u + splits);
+      __builtin_amdgcn_sched_barrier(0);  // loads stay where they are
+    }
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            x[t][j] = (f32x4){};
-            if (in) x[t][j] = *reinterpret_cast<const f32x4*>(static_cast<const float*>(a.x) + x_row[t] + k + i * 8 + j * 4);
-          }
-        const f32x2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[i], s, 0), q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[i], s, 1);
-        const f32x2 r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[i], s, 2), u = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[i], s, 3);
-        const float y[8] = {p[0], p[1], q[0], q[1], r[0], r[1], u[0], u[1]};
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-          for (int t = 0; t < NT; ++t) acc[t] = Mfma<16>::mul(y[j], x[t][j >> 2][j & 3], acc[t]);
+    for (int i = 0; i < 4; ++i) {
+      multiply(i, buf, false);
+      if constexpr (more) {
+        load_c(u + splits, i);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+    buf ^= 1;
+    if constexpr (more) {
+      stage(buf);
+      e = e_next;
+    }
+  };
+  if (turns > 0) {
+    int u = ks;
+    load_x(u);
+    __builtin_memcpy(&e, exps + u * kUnitGroups, 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load_c(u, i);
+    stage(0);
+    for (int t = 1; t < turns; ++t, u += splits) unit(u, std::true_type{});
+    unit(u, std::false_type{});
   }
+  // what is left: fewer units than splits, the last one perhaps of fewer groups
+  if (turns * splits < units) {
+    const int u = turns * splits + ks, at = min(u, units - 1);
+    load_x(at);
 #pragma unroll
-  for (int t = 0; t < NT; ++t) parts[wave][t][lane] = acc[t];
+    for (int i = 0; i < 4; ++i) {
+      const int g = min(at * kUnitGroups + i * 4 + grp, groups - 1);
+      c[i] = *reinterpret_cast<const u32x4*>(w + (long)g * 16);
+      e[i] = (unsigned)(uint8_t)exps[g] << (8 * grp);
+    }
+    stage(buf);
+    meet();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) multiply(i, buf, u * kUnitGroups + i * 4 + grp >= groups);  // inputs of 0 past the last
+  }
   __syncthreads();
-  // acc[e] of a lane: output o0 + grp * 4 + e of row l16 of the tile
-  for (int f = threadIdx.x; f < NT * kWave; f += kWaves * kWave) {
-    const int t = f / kWave, l = f % kWave;
-    const int m = m0 + t * kOuts + (l & 15), o = o0 + (l >> 4) * 4;
-    if (m >= a.rows) continue;
-    f32x4 sum = parts[0][t][l];
+
+  // the splits' sums. acc[t][e]: output o0 + no * 16 + grp * 4 + e, column l16 of tile t
+  f32x4* parts = reinterpret_cast<f32x4*>(lds);
 #pragma unroll
-    for (int x = 1; x < kWaves; ++x) sum += parts[x][t][l];
+  for (int t = 0; t < NT; ++t) parts[(wave * NT + t) * kWave + lane] = acc[t];
+  __syncthreads();
+  constexpr int PER = BF16 ? kOuts : 5;  // rows of a tile
+  for (int f = threadIdx.x; f < outs * NT * 4 * PER; f += blockDim.x) {
+    const int tile = f / (4 * PER), slot = f / PER % 4, r = f % PER;
+    const int m = m0 + tile % NT * PER + r, o = o0 + tile / NT * kOuts + slot * 4;
+    if (m >= a.rows) continue;
+    f32x4 sum = {};
+    for (int x = 0; x < splits; ++x)
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) sum += parts[(x * outs * NT + tile) * kWave + slot * kOuts + r * PARTS + p];
     if (a.row_scale) sum *= a.row_scale[m];
     const long at = (long)m * a.d_out + o;
 #pragma unroll
@@ -119,19 +222,67 @@ __global__ __launch_bounds__(kWaves * kWave) void linear_w4_kernel(LinearW4 a) {
   }
 }
 
-template <bool BF16, int NT>
-hipError_t launch(const LinearW4& a, hipStream_t s) {
-  const unsigned outs = (unsigned)((a.d_out + kOuts - 1) / kOuts), rows = (unsigned)((a.rows + NT * kOuts - 1) / (NT * kOuts));
-  hipLaunchKernelGGL((linear_w4_kernel<BF16, NT>), dim3(outs, rows), dim3(kWaves * kWave), 0, s, a);
+template <bool BF16, int NT, int XS>
+hipError_t launch(const LinearW4& a, int outs, int splits, hipStream_t s) {
+  constexpr int ROWS = NT * (BF16 ? kOuts : 5);
+  const unsigned wgs = (unsigned)((a.d_out + outs * kOuts - 1) / (outs * kOuts)), tiles = (unsigned)((a.rows + ROWS - 1) / ROWS);
+  const int lds = std::max(splits * 2 * XS * outs * (BF16 ? 1 : 3), outs * splits * NT) * 1024;
+  hipLaunchKernelGGL((linear_w4_kernel<BF16, NT, XS>), dim3(wgs, tiles), dim3(outs * splits * kWave), lds, s, a, outs, splits);
   return hipGetLastError();
+}
+
+template <int NT>
+hipError_t launch_bf16(const LinearW4& a, int outs, int splits, hipStream_t s) {
+  const int per = (std::min(a.rows, NT * kOuts) + outs - 1) / outs;  // rows of x for each wave
+  if (per <= 1) return launch<true, NT, 1>(a, outs, splits, s);
+  if (per <= 2) return launch<true, NT, 2>(a, outs, splits, s);
+  if (per <= 4) return launch<true, NT, 4>(a, outs, splits, s);
+  if (NT > 1 || per <= 8) return launch<true, NT, 8>(a, outs, splits, s);
+  return launch<true, NT, 16>(a, outs, splits, s);
+}
+
+template <int NT>
+hipError_t launch_f32(const LinearW4& a, int outs, int splits, hipStream_t s) {
+  const int per = (std::min(a.rows, NT * 5) + outs - 1) / outs;
+  if (per <= 1) return launch<false, NT, 1>(a, outs, splits, s);
+  if (per <= 2) return launch<false, NT, 2>(a, outs, splits, s);
+  if (per <= 3) return launch<false, NT, 3>(a, outs, splits, s);
+  return launch<false, NT, 5>(a, outs, splits, s);
 }
 
 }  // namespace
 
+// Tiles of rows, waves that share inputs and waves that share outputs: as many of the former as leave a workgroup
+// for each CU, for they share what is read of x, and the latter where there is enough to split. us:
+//                          1x4  2x2  4x1  4x2  8x1             2 tiles 4x1  8x1   4 tiles 8x1
+//    4 rows, 8960 x 1536   6.6  8.5 12.7 12.6 22.5
+//    4       5120 x 5120   9.2  7.4 10.9 10.3 18.2
+//   16       1536 x 8960   9.8  6.6  5.3  6.7  6.9
+//   16       8192 x 32768   64   39   38   38   37
+//   32       5120 x 16384                  22   21                   18     25       28
+//   32       8192 x 32768             63   63   58                   45     42       49
+//   64       5120 x 16384             37   36   33                   27     24       35
+//   64       8192 x 32768            112  112  102                   78     67       56
 hipError_t launch_linear_w4(const LinearW4& a, bool bf16, hipStream_t s) {
   if (a.rows <= 0 || a.d_out <= 0) return hipSuccess;
-  if (bf16) return a.rows <= 16 ? launch<true, 1>(a, s) : a.rows <= 32 ? launch<true, 2>(a, s) : launch<true, 4>(a, s);
-  return a.rows <= 16 ? launch<false, 1>(a, s) : launch<false, 2>(a, s);
+  const long outs = (a.d_out + kOuts - 1) / kOuts, cus = compute_units();
+  const int units = (a.d_in + kUnit - 1) / kUnit;
+  const bool many = outs >= 2 * cus, some = outs >= cus;
+  const int four = units >= 8 ? 2 : 1, two = units >= 2 ? 2 : 1, one = std::min(units, 4);  // splits beside 4, 2 and 1
+  if (!bf16) {
+    if (a.rows > 10 && outs >= 4 * cus) return launch_f32<4>(a, 4, 1, s);
+    if (many || (some && a.rows > 5)) return launch_f32<1>(a, 4, four, s);
+    return some ? launch_f32<1>(a, 2, two, s) : launch_f32<1>(a, 1, one, s);
+  }
+  if (a.rows > 16) {
+    if (many) {
+      if (outs < 8 * cus) return launch_bf16<2>(a, a.rows <= 32 ? 4 : 8, 1, s);
+      return a.rows <= 32 ? launch_bf16<2>(a, 8, 1, s) : launch_bf16<4>(a, 8, 1, s);
+    }
+    return some ? launch_bf16<1>(a, 4, 1, s) : launch_bf16<1>(a, 2, two, s);
+  }
+  if (many) return launch_bf16<1>(a, 4, four, s);
+  return some ? launch_bf16<1>(a, 2, two, s) : launch_bf16<1>(a, 1, one, s);
 }
 
 }  // namespace hsa
