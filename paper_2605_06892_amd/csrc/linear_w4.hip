@@ -35,32 +35,6 @@ __device__ __forceinline__ float gelu_exact(float x) {
   return x / (1.f + expf(-2.f * y));
 }
 
-// 8 codes of a word as bf16, times a power of two
-__device__ __forceinline__ bf16x8 widen8(unsigned c, float scale) {
-  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1);
-  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2), t = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3);
-  return (bf16x8){p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
-}
-
-// The three bf16 parts of 8 fp32 values. What is not finite is its first part alone.
-__device__ __forceinline__ void cut(const u32x4 (&x)[2], u32x4 (&part)[3]) {
-  unsigned h[8], m[8], l[8];
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const unsigned u = x[j >> 2][j & 3], mag = u & 0x7fffffffu;
-    h[j] = (u & 0xffff0000u) | (mag > 0x7f800000u ? 0x00400000u : 0u);
-    const float r = mag < 0x7f800000u ? __uint_as_float(u) - __uint_as_float(h[j]) : 0.f;
-    m[j] = __float_as_uint(r);
-    l[j] = __float_as_uint(r - __uint_as_float(m[j] & 0xffff0000u));
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {  // the upper halves of two
-    part[0][j] = __builtin_amdgcn_perm(h[2 * j + 1], h[2 * j], 0x07060302);
-    part[1][j] = __builtin_amdgcn_perm(m[2 * j + 1], m[2 * j], 0x07060302);
-    part[2][j] = __builtin_amdgcn_perm(l[2 * j + 1], l[2 * j], 0x07060302);
-  }
-}
-
 // Workgroups of splits * outs waves; NT tiles of rows of x; XS rows of x loaded by each wave of a split.
 template <bool BF16, int NT, int XS>
 __global__ __launch_bounds__(kMostWaves * kWave) void linear_w4_kernel(LinearW4 a, int outs, int splits) {
@@ -95,13 +69,19 @@ __global__ __launch_bounds__(kMostWaves * kWave) void linear_w4_kernel(LinearW4 
   auto stage = [&](int buf) {
 #pragma unroll
     for (int i = 0; i < XS; ++i) {
-      u32x4 part[PARTS];
-      if constexpr (BF16) part[0] = xr[i][0];
-      else cut(xr[i], part);
+      bf16x8 part[PARTS];
+      if constexpr (BF16) {
+        part[0] = __builtin_bit_cast(bf16x8, xr[i][0]);
+      } else {
+        float x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(xr[i][j >> 2][j & 3]);
+        cut3(x, part);
+      }
 #pragma unroll
       for (int p = 0; p < PARTS; ++p) {
         const int r = (i * outs + no) * PARTS + p;
-        *reinterpret_cast<u32x4*>(xl + (buf * x_rows + r) * 1024 + (lane ^ (r & 7)) * 16) = part[p];
+        *reinterpret_cast<bf16x8*>(xl + (buf * x_rows + r) * 1024 + (lane ^ (r & 7)) * 16) = part[p];
       }
     }
   };
@@ -128,7 +108,7 @@ __global__ __launch_bounds__(kMostWaves * kWave) void linear_w4_kernel(LinearW4 
     const float s = pow2((int8_t)(e[i] >> (8 * grp)));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const bf16x8 y = widen8(c[i][j], s);
+      const bf16x8 y = widen4(c[i][j], s);
 #pragma unroll
       for (int t = 0; t < NT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, x[t][j], acc[t], 0, 0, 0);
     }

@@ -24,156 +24,43 @@
 //          without a rounding (4 significant bits and a power of two).
 //   fp32   16x16x4: K and V rows both in their operand's layout.
 // Probabilities are rounded to bf16 in the bf16 form; the sums take them before that.
-#include "seq_common.h"
-
-#include <algorithm>
+#include "paged.h"
 
 namespace hsa {
 namespace {
 
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr int kTile = 128;       // rows of a tile
-constexpr int kRows = 16;        // query heads of an item
 constexpr int kSplitWaves = 4, kWholeWaves = 8;
-constexpr int kMaxGroups = 1024;
-constexpr int kJoinThreads = 256;
-
-struct Plan {
-  int wgs;        // workgroups that the tiles are dealt to
-  int gts;        // items per (sequence, key/value head)
-  FastDiv page;
-};
-
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-
-__device__ __forceinline__ int seq_len(const PagedArgs& a, int s) {
-  const long most = a.n_pages > 0 ? (long)a.max_pages * a.page_size : 0;
-  const int len = max(a.kv_lens[s], 0);
-  return len > most ? (int)most : len;
-}
-// tiles of a sequence (one for an empty one: its output is written too)
-__device__ __forceinline__ int tiles_of(int len) { return max((len + kTile - 1) / kTile, 1); }
-
-// x / y for non-negative values, in 32 bits where they fit
-__device__ __forceinline__ long div_pos(long x, long y) {
-  return (x | y) >> 31 ? x / y : (long)((unsigned)x / (unsigned)y);
-}
-
-// The tiles of all items in order: sequence by sequence, in it head by head. A
-// wave's view: 64 sequences at a time, the whole batch at once where it has no more.
-struct Walk {
-  int s0;           // first sequence in view
-  int len;          // of sequence s0 + lane
-  long before;      // tiles before s0
-  long from, upto;  // tiles before and up to the end of this lane's sequence
-
-  __device__ __forceinline__ void view(const PagedArgs& a, int per, int first, long tiles_before) {
-    const int lane = threadIdx.x & (kWave - 1);
-    s0 = first;
-    before = tiles_before;
-    len = s0 + lane < a.n_seqs ? seq_len(a, s0 + lane) : 0;
-    const long n = s0 + lane < a.n_seqs ? (long)tiles_of(len) * per : 0;
-    upto = n;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const long y = __shfl_up(upto, o);
-      if (lane >= o) upto += y;
-    }
-    upto += before;
-    from = upto - n;
-  }
-  __device__ __forceinline__ long end() const { return __shfl(upto, kWave - 1); }
-  // Lane whose sequence holds tile `at`, moving the view on to it; -1 past the last sequence.
-  __device__ __forceinline__ int find(const PagedArgs& a, int per, long at) {
-    for (;;) {
-      const unsigned long hit = __ballot(from <= at && at < upto);
-      if (hit) return __builtin_ctzl(hit);
-      if (s0 + kWave >= a.n_seqs) return -1;
-      view(a, per, s0 + kWave, end());
-    }
-  }
-};
-
-// tiles of all items
-__device__ __forceinline__ long all_tiles(const PagedArgs& a, int per, const Walk& first) {
-  if (a.n_seqs <= kWave) return first.end();
-  long sum = 0;
-  for (int s = threadIdx.x & (kWave - 1); s < a.n_seqs; s += kWave) sum += tiles_of(seq_len(a, s));
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-  return sum * per;
-}
-// tiles of a run
-__device__ __forceinline__ long run_tiles(long total, int wgs) { return div_pos(total + wgs - 1, wgs); }
-
-template <int DH>
-struct Part {  // a part of an item in the workspace
-  float o[kRows * DH];
-  float ml[kRows * 2];
-};
-// The item that a run begins and does not end: its parts are this run's in
-// `slot` and the next `more` runs' first (0: there is no such item). In the workspace
-// behind the parts, two to a run.
-struct Note {
-  int s, item, slot, more;
-};
-template <int DH>
-__device__ __forceinline__ Note* notes(const PagedArgs& a, const Plan& plan) {
-  return reinterpret_cast<Note*>(static_cast<Part<DH>*>(a.ws) + 2 * (long)plan.wgs);
-}
-
-// exp((x - y) * scale) for x <= y, as exact as the form needs
-template <bool F32>
-__device__ __forceinline__ float rescale(float x, float y, float scale) {
-  return F32 ? expf((x - y) * scale) : __builtin_amdgcn_exp2f((x - y) * (scale * kLog2e));
-}
-
-// 4 channels (from c) of query head `orow` of all, and with c == 0 its lse, from
-// the softmax's maximum, sum and weighted values
-template <bool F32, int DH>
-__device__ __forceinline__ void write_out(const PagedArgs& a, long orow, int c, float m, float l, f32x4 sum) {
-  sum *= l == 0.f ? 0.f : 1.f / l;
-  if constexpr (F32) *reinterpret_cast<f32x4u*>(static_cast<float*>(a.o) + orow * DH + c) = sum;
-  else *reinterpret_cast<bf16x4*>(static_cast<bf16*>(a.o) + orow * DH + c) = to_bf16x4(sum);
-  if (a.lse && c == 0) a.lse[orow] = l == 0.f ? -INFINITY : fmaf(m, a.scale, logf(l));
-}
 
 // One item, or the rows key0 .. key1-1 of one, by NW waves.
-template <bool F32, Held HELD, int DH, bool ALIGNED, int NW>
+template <bool F32, bool E4M3, int DH, bool ALIGNED, int NW>
 struct Attend {
-  static constexpr bool E4M3 = HELD == kE4M3, E2M1 = HELD == kE2M1, EXPS = E4M3 || E2M1;
-  static constexpr bool VREG = F32 || E2M1;       // V goes from its loads to the products without LDS
   static constexpr int BK = F32 ? 16 : 32;        // keys per block
   static constexpr int KT = BK / 16;              // key tiles of a block
   static constexpr int DT = DH / 16;              // channel tiles of O^T
   static constexpr int P = DH + 4;                // padded row of the merge buffer, floats
-  static constexpr int BITS = E2M1 ? 4 : E4M3 ? 8 : (F32 ? 32 : 16);
-  static constexpr int HB = DH * BITS / 8;        // bytes of a head's row
-  static constexpr int HX = E2M1 ? DH / kGroup : 1;  // its exponents
-  static constexpr int CB = E2M1 ? HB / 4 : 16;   // bytes of a load
-  static constexpr int CE = CB * 8 / BITS;        // values of a load
+  static constexpr int ES = E4M3 ? 1 : (F32 ? 4 : 2);
+  static constexpr int CB = 16;                   // bytes of a load
+  static constexpr int CE = CB / ES;              // values of a load
   static constexpr int KL = DH / CE / 4;          // K loads per lane and key tile (its 4 slots share a row)
-  // V: in the bf16 form whole rows over the wave; where it stays in registers DT consecutive
-  // channels of the keys of a slot (4 of each key tile)
-  static constexpr int VR = VREG ? 4 * KT : BK * DH / CE / 64;
-  static constexpr int VB = VREG ? DT * BITS / 8 : CB;  // bytes of one V read
+  // V: bf16 form, whole rows over the wave; fp32 form, DT consecutive channels of the 4 keys of a slot
+  static constexpr int VR = F32 ? 4 : BK * DH / CE / 64;
+  static constexpr int VB = F32 ? DT * ES : CB;   // bytes of one V read
   static constexpr int CPR = DH / CE;             // loads per row
   static constexpr unsigned kAll = BK == 32 ? ~0u : 0xffffu;
   struct VLoad { unsigned char b[VB]; };
-  struct KLoad { unsigned w[CB / 4]; };
   struct Shared {
     float buf[NW][kRows * P];  // V rows, then the merge
     float m_part[NW][kRows], l_part[NW][kRows];
   };
-  static_assert(VREG || kRows * P * 4 >= BK * DH * 2, "a block's V rows fit");
+  static_assert(F32 || kRows * P * 4 >= BK * DH * 2, "a block's V rows fit");
 
   // The bf16 form loads whole rows of V, which nothing reads again: past the caches. K, whose rows
   // several loads share, stays (four sequences of 30011 to 131072: 226 us, V past the
   // caches 216, both 238).
   static __device__ __forceinline__ void load_v(VLoad& v, const char* p) {
-    if constexpr (VREG) {
+    if constexpr (F32) {
       __builtin_memcpy(&v, p, VB);
     } else {
       const u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
@@ -193,19 +80,6 @@ struct Attend {
     return y;
   }
 
-  // 8 codes of a word as fp32, times a power of two
-  static __device__ __forceinline__ void x8(float (&x)[8], unsigned c, float scale) {
-    const f32x2 p = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 0), q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 1);
-    const f32x2 r = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 2), t = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, 3);
-    x[0] = p[0], x[1] = p[1], x[2] = q[0], x[3] = q[1], x[4] = r[0], x[5] = r[1], x[6] = t[0], x[7] = t[1];
-  }
-  // 8 codes of a word as bf16, times a power of two: exact
-  static __device__ __forceinline__ bf16x8 widen4(unsigned c, float scale) {
-    const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1);
-    const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2), t = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3);
-    return (bf16x8){p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
-  }
-
   // s, h, g0 (first query head of the group), key0 and key1 are uniform. part:
   // where the unnormalized result goes, NULL for the output itself.
   static __device__ __forceinline__ void run(const PagedArgs& a, const Plan& plan, Shared& sh, int s, int h, int g0,
@@ -213,7 +87,7 @@ struct Attend {
     const int lane = threadIdx.x & 63;
     const int wave = uniform(threadIdx.x >> 6);
     const int l16 = lane & 15, grp = lane >> 4;
-    const unsigned row_bytes = (unsigned)a.kv_heads * HB, row_exps = (unsigned)a.kv_heads * HX;
+    const unsigned row_bytes = (unsigned)(a.kv_heads * DH) * ES;
     const float sl2e = a.scale * kLog2e;
     const int32_t* pages = a.page_table + (long)s * a.max_pages;
     bf16* vl = reinterpret_cast<bf16*>(sh.buf[wave]);
@@ -223,7 +97,7 @@ struct Attend {
 
     // one block ahead: its rows (as held), exponents, and which of its keys exist;
     // two blocks ahead: the page of this lane's key (lane % BK; ALIGNED: of all keys)
-    KLoad kr[KT][KL];
+    u32x4 kr[KT][KL];
     VLoad vr[VR];
     int ke[KT], ve[VR];
     unsigned mask = 0;
@@ -233,12 +107,10 @@ struct Attend {
       page = -1;
       if (t < key1) page = pages[plan.page.quot(t)];
     };
-    auto v_key = [&](int i) { return VREG ? grp * 4 + (i & 3) + (i >> 2) * 16 : (i * 64 + lane) / CPR; };
+    auto v_key = [&](int i) { return F32 ? grp * 4 + i : (i * 64 + lane) / CPR; };
     // byte offsets of this lane's loads in a block's rows, where those are consecutive
     const unsigned k_off = l16 * row_bytes + grp * CB;
-    const unsigned v_off = VREG ? (unsigned)grp * 4 * row_bytes + l16 * VB : (lane / CPR) * row_bytes + lane % CPR * CB;
-    // exponents of the channels of this lane's loads
-    const unsigned k_x = E2M1 ? grp * (DH / 4) / kGroup : 0, v_x = E2M1 ? l16 * DT / kGroup : 0;
+    const unsigned v_off = F32 ? (unsigned)grp * 4 * row_bytes + l16 * VB : (lane / CPR) * row_bytes + lane % CPR * CB;
     auto load = [&](int n0) {
       if (n0 >= key1) return;
       const int t = n0 + (ALIGNED ? 0 : lane % BK);
@@ -248,37 +120,37 @@ struct Attend {
       if constexpr (ALIGNED) {  // a block lies in one page: rows first ..
         first = uniform(first);
         load_page(n0 + NW * BK);
-        const char* kb = static_cast<const char*>(a.k) + (long)first * row_bytes + h * HB;
-        const char* vb = static_cast<const char*>(a.v) + (long)first * row_bytes + h * HB;
-        const int8_t* keb = a.k_exp + (long)first * row_exps + h * HX;
-        const int8_t* veb = a.v_exp + (long)first * row_exps + h * HX;
+        const char* kb = static_cast<const char*>(a.k) + (long)first * row_bytes + h * (DH * ES);
+        const char* vb = static_cast<const char*>(a.v) + (long)first * row_bytes + h * (DH * ES);
+        const int8_t* keb = a.k_exp + (long)first * a.kv_heads + h;
+        const int8_t* veb = a.v_exp + (long)first * a.kv_heads + h;
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
 #pragma unroll
           for (int i = 0; i < KL; ++i) __builtin_memcpy(&kr[kt][i], kb + (kt * 16 * row_bytes + k_off + i * 4 * CB), CB);
-          if constexpr (EXPS) ke[kt] = keb[(unsigned)(kt * 16 + l16) * row_exps + k_x];
+          if constexpr (E4M3) ke[kt] = keb[(unsigned)(kt * 16 + l16) * a.kv_heads];
         }
 #pragma unroll
         for (int i = 0; i < VR; ++i) {
-          load_v(vr[i], vb + ((VREG ? (i & 3) + (i >> 2) * 16 : i * 64 / CPR) * row_bytes + v_off));
-          if constexpr (EXPS) ve[i] = veb[(unsigned)v_key(i) * row_exps + v_x];
+          load_v(vr[i], vb + ((F32 ? i : i * 64 / CPR) * row_bytes + v_off));
+          if constexpr (E4M3) ve[i] = veb[(unsigned)v_key(i) * a.kv_heads];
         }
       } else {
         load_page(n0 + NW * BK);
 #pragma unroll
         for (int kt = 0; kt < KT; ++kt) {
           const long r = __shfl(first, kt * 16 + l16);
-          const char* src = static_cast<const char*>(a.k) + r * row_bytes + h * HB + grp * CB;
+          const char* src = static_cast<const char*>(a.k) + r * row_bytes + h * (DH * ES) + grp * CB;
 #pragma unroll
           for (int i = 0; i < KL; ++i) __builtin_memcpy(&kr[kt][i], src + i * 4 * CB, CB);
-          if constexpr (EXPS) ke[kt] = a.k_exp[r * row_exps + h * HX + k_x];
+          if constexpr (E4M3) ke[kt] = a.k_exp[r * a.kv_heads + h];
         }
 #pragma unroll
         for (int i = 0; i < VR; ++i) {
           const long r = __shfl(first, v_key(i));
-          const unsigned c = VREG ? l16 * VB : lane % CPR * CB;
-          load_v(vr[i], static_cast<const char*>(a.v) + r * row_bytes + h * HB + c);
-          if constexpr (EXPS) ve[i] = a.v_exp[r * row_exps + h * HX + v_x];
+          const unsigned c = F32 ? l16 * VB : lane % CPR * CB;
+          load_v(vr[i], static_cast<const char*>(a.v) + r * row_bytes + h * (DH * ES) + c);
+          if constexpr (E4M3) ve[i] = a.v_exp[r * a.kv_heads + h];
         }
       }
     };
@@ -318,35 +190,25 @@ struct Attend {
       float vf[F32 ? 4 : 1][DT];
       if constexpr (F32) {
         // codes times their exponent before the products, which could overflow without it
-        const float sk = EXPS ? pow2(ke[0]) : 1.f;
+        const float sk = E4M3 ? pow2(ke[0]) : 1.f;
 #pragma unroll
         for (int i = 0; i < KL; ++i)
 #pragma unroll
-          for (int j = 0; j < CB / 4; ++j) {
-            constexpr int N = 32 / BITS;  // values of a word
-            float x[N];
-            if constexpr (E2M1) {
-              x8(x, kr[0][i].w[j], sk);
-            } else if constexpr (E4M3) {
-              const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)kr[0][i].w[j], false);
-              const f32x2 up = __builtin_amdgcn_cvt_pk_f32_fp8((int)kr[0][i].w[j], true);
+          for (int j = 0; j < 4; ++j) {
+            float x[CE / 4];
+            if constexpr (E4M3) {
+              const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)kr[0][i][j], false);
+              const f32x2 up = __builtin_amdgcn_cvt_pk_f32_fp8((int)kr[0][i][j], true);
               x[0] = lo[0] * sk, x[1] = lo[1] * sk, x[2] = up[0] * sk, x[3] = up[1] * sk;
             } else {
-              x[0] = __uint_as_float(kr[0][i].w[j]);
+              x[0] = __uint_as_float(kr[0][i][j]);
             }
 #pragma unroll
-            for (int u = 0; u < N; ++u) sc[0] = Mfma<16>::mul(x[u], qs[i * CE + j * N + u], sc[0]);
+            for (int u = 0; u < CE / 4; ++u) sc[0] = Mfma<16>::mul(x[u], qs[i * CE + j * (CE / 4) + u], sc[0]);
           }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if constexpr (E2M1) {
-            unsigned c = 0;
-            __builtin_memcpy(&c, &vr[i], VB);
-            float x[8];
-            x8(x, c, pow2(ve[i]));
-#pragma unroll
-            for (int dt = 0; dt < DT; ++dt) vf[i][dt] = x[dt];
-          } else if constexpr (E4M3) {
+          if constexpr (E4M3) {
             const float sv = pow2(ve[i]);
 #pragma unroll
             for (int j = 0; j < DT / 4; ++j) {
@@ -365,7 +227,6 @@ struct Attend {
             for (int dt = 0; dt < DT; ++dt) vf[i][dt] = 0.f;
         }
       } else {
-        if constexpr (!VREG)
 #pragma unroll
         for (int i = 0; i < VR; ++i) {
           const int f = i * 64 + lane, r = f / CPR;
@@ -387,40 +248,17 @@ struct Attend {
         for (int i = 0; i < KL; ++i)
 #pragma unroll
           for (int kt = 0; kt < KT; ++kt) {
-            if constexpr (E2M1) {
-              const float sk = pow2(ke[kt]);
-#pragma unroll
-              for (int j = 0; j < CB / 4; ++j)
-                sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen4(kr[kt][i].w[j], sk), qb[i * (CE / 8) + j], sc[kt], 0, 0, 0);
-            } else if constexpr (E4M3) {
+            if constexpr (E4M3) {
               const float sk = pow2(ke[kt]);
 #pragma unroll
               for (int j = 0; j < 2; ++j)
-                sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(kr[kt][i].w[2 * j], kr[kt][i].w[2 * j + 1], sk),
+                sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(kr[kt][i][2 * j], kr[kt][i][2 * j + 1], sk),
                                                                  qb[i * 2 + j], sc[kt], 0, 0, 0);
             } else {
               sc[kt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kr[kt][i]), qb[i], sc[kt], 0, 0, 0);
             }
           }
-        if constexpr (!VREG) __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");  // the V rows are in LDS
-      }
-      // V of the slot's 8 keys, two channels of a tile pair each
-      bf16x2 v2[E2M1 && !F32 ? DT / 2 : 1][8];
-      if constexpr (E2M1 && !F32) {
-#pragma unroll
-        for (int i = 0; i < VR; ++i) {
-          unsigned c = 0;
-          __builtin_memcpy(&c, &vr[i], VB);
-          int e = ve[i];
-          if (cut && !(keys >> v_key(i) & 1)) c = 0, e = 0;  // neither codes nor exponents of rows that are not there
-          const float sv = pow2(e);
-          v2[0][i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, sv, 0);
-          v2[1][i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, sv, 1);
-          if constexpr (DT == 8) {
-            v2[2][i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, sv, 2);
-            v2[3][i] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, sv, 3);
-          }
-        }
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");  // the V rows are in LDS
       }
       load(n0 + NW * BK);
 
@@ -462,15 +300,6 @@ struct Attend {
       } else {
         const bf16x8 pf = __builtin_shufflevector(to_bf16x4(sc[0]), to_bf16x4(sc[KT - 1]), 0, 1, 2, 3, 4, 5, 6, 7);
         const int r = grp * 4 + (l16 >> 2);
-        if constexpr (E2M1) {
-#pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            bf16x8 vf8;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) vf8[i] = v2[dt / 2][i][dt & 1];
-            acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf8, pf, acc[dt], 0, 0, 0);
-          }
-        } else
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
           const int col = dt * 16 + 4 * (lane & 3);
@@ -480,12 +309,12 @@ struct Attend {
           acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7), pf,
                                                             acc[dt], 0, 0, 0);
         }
-        if constexpr (!VREG) __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");  // read before the next block's rows
+        __builtin_amdgcn_fence(__ATOMIC_SEQ_CST, "wavefront");  // read before the next block's rows
       }
     }
 
     // merge of the waves. acc[dt][e] is channel dt*16 + grp*4 + e of row l16,
-    // where V stays in registers (grp*4 + e)*DT + dt
+    // in the fp32 form (grp*4 + e)*DT + dt
     float l_tot = l_run + __shfl_xor(l_run, 16);
     l_tot += __shfl_xor(l_tot, 32);
     if (grp == 0) {
@@ -494,7 +323,7 @@ struct Attend {
     }
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt) {
-      if constexpr (VREG) {
+      if constexpr (F32) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) sh.buf[wave][l16 * P + (grp * 4 + e) * DT + dt] = acc[dt][e];
       } else {
@@ -529,9 +358,9 @@ struct Attend {
 };
 
 // one item per workgroup
-template <bool F32, Held HELD, int DH, bool ALIGNED>
+template <bool F32, bool E4M3, int DH, bool ALIGNED>
 __global__ __launch_bounds__(kWholeWaves * 64) void paged_whole_kernel(PagedArgs a, Plan plan) {
-  typedef Attend<F32, HELD, DH, ALIGNED, kWholeWaves> A;
+  typedef Attend<F32, E4M3, DH, ALIGNED, kWholeWaves> A;
   __shared__ __attribute__((aligned(16))) typename A::Shared sh;
   const int per = a.kv_heads * plan.gts;
   const int s = blockIdx.x / per, item = blockIdx.x - s * per, h = item / plan.gts;
@@ -541,9 +370,9 @@ __global__ __launch_bounds__(kWholeWaves * 64) void paged_whole_kernel(PagedArgs
 // One run of tiles per workgroup. Two waves to a SIMD, stated: without it the
 // compiler spreads the 128-wide forms over more registers than that leaves (48
 // sequences of 201 to 8009 rows in bf16 94 -> 85 us).
-template <bool F32, Held HELD, int DH, bool ALIGNED>
+template <bool F32, bool E4M3, int DH, bool ALIGNED>
 __global__ __launch_bounds__(kSplitWaves * 64, 2) void paged_split_kernel(PagedArgs a, Plan plan) {
-  typedef Attend<F32, HELD, DH, ALIGNED, kSplitWaves> A;
+  typedef Attend<F32, E4M3, DH, ALIGNED, kSplitWaves> A;
   __shared__ __attribute__((aligned(16))) typename A::Shared sh;
   const int per = a.kv_heads * plan.gts;
   Walk walk;
@@ -571,101 +400,17 @@ __global__ __launch_bounds__(kSplitWaves * 64, 2) void paged_split_kernel(PagedA
   if (threadIdx.x == 0) notes<DH>(a, plan)[blockIdx.x] = note;
 }
 
-// The output of the item that run blockIdx.x begins and does not end, one query
-// head per workgroup: its threads take 4 channels each of every few parts, then join those.
-template <bool F32, int DH>
-__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a, Plan plan) {
-  constexpr int C = DH / 4, G = kJoinThreads / C;  // threads per part, parts at a time
-  __shared__ __attribute__((aligned(16))) f32x4 sums[G][C];
-  __shared__ float ms[G], ls[G];
-  const int w0 = blockIdx.x, r = blockIdx.y;
-  const Note note = notes<DH>(a, plan)[w0];
-  const int h = note.item / plan.gts, g = (note.item - h * plan.gts) * kRows + r;
-  if (note.more == 0 || g >= a.group) return;
-  const Part<DH>* parts = static_cast<const Part<DH>*>(a.ws);
-  const int lane_p = threadIdx.x / C, c = (threadIdx.x - lane_p * C) * 4;
-  float m = -INFINITY, l = 0.f;
-  f32x4 sum = {};
-  constexpr int U = 4;  // parts loaded at once by each
-  for (int i0 = lane_p; i0 <= note.more; i0 += U * G) {
-    f32x2 ml[U];
-    f32x4 x[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = min(i0 + u * G, note.more);
-      const Part<DH>* p = parts + 2 * (long)(w0 + i) + (i ? 0 : note.slot);
-      ml[u] = *reinterpret_cast<const f32x2*>(&p->ml[2 * r]);
-      x[u] = *reinterpret_cast<const f32x4*>(&p->o[r * DH + c]);
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i0 + u * G > note.more || (ml[u][0] == -INFINITY && ml[u][1] == 0.f)) continue;  // no key, or no finite score
-      const float m_new = fmaxf(m, ml[u][0]);
-      const float was = m == -INFINITY ? 0.f : rescale<F32>(m, m_new, a.scale), wt = rescale<F32>(ml[u][0], m_new, a.scale);
-      m = m_new;
-      l = fmaf(wt, ml[u][1], l * was);
-      sum = sum * was + wt * x[u];
-    }
-  }
-  sums[lane_p][c / 4] = sum;
-  if (c == 0) {
-    ms[lane_p] = m;
-    ls[lane_p] = l;
-  }
-  __syncthreads();
-  if (lane_p > 0) return;
-  float m_all = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < G; ++i) m_all = fmaxf(m_all, ms[i]);
-  l = 0.f;
-  sum = (f32x4){};
-#pragma unroll
-  for (int i = 0; i < G; ++i) {
-    if (ms[i] == -INFINITY && ls[i] == 0.f) continue;
-    const float wt = rescale<F32>(ms[i], m_all, a.scale);
-    l = fmaf(wt, ls[i], l);
-    sum += wt * sums[i][c / 4];
-  }
-  write_out<F32, DH>(a, (long)note.s * (a.kv_heads * a.group) + h * a.group + g, c, m_all, l, sum);
-}
-
-int gts_of(int group) { return (group + kRows - 1) / kRows; }
-
-// Rows up to which an item is one workgroup's. Dealing out tiles costs the walk and the join
-// (4 to 5 us), a whole item the time of its rows in one workgroup, and the fewer items, the
-// fewer CUs share that. Whole and dealt, us, bf16, 128 channels, batches of half to full length:
-//     8 items    700 rows 11.1  9.8    1000 14.6  9.7    1500 19.9 10.1
-//    64          700      11.8 11.8    1000 15.7 12.6    1500 21.3 16.2
-//   128         1000      16.7 19.1    1250 19.4 19.3    2000 28.0 25.4
-//   256         1000      20.6 26.0    2000 35.7 38.3    4000 73.5 75.4
-// (64 channels and e4m3 cross within a third of these.)
-constexpr long kLeastWhole = 768;
-long whole_len(long items) {
-  const int cus = compute_units();
-  return items * 4 <= cus ? kLeastWhole : items * 2 <= cus ? 1024 : 2048;
-}
-bool splits(int n_seqs, int kv_heads, int group, long max_len) {
-  return max_len > whole_len((long)n_seqs * kv_heads * gts_of(group));
-}
-
-// Workgroups the tiles are dealt to: as many as run at once, no more than tiles
-// if every sequence is as long as it may be.
-int workgroups(int n_seqs, int kv_heads, int group, long max_len) {
-  const long tiles = (long)n_seqs * kv_heads * gts_of(group) * ((max_len + kTile - 1) / kTile);
-  return (int)std::min(std::min((long)kMaxGroups, 2L * compute_units()), tiles);
-}
-
-template <bool F32, Held HELD, int DH, bool ALIGNED>
+template <bool F32, bool E4M3, int DH, bool ALIGNED>
 hipError_t launch(const PagedArgs& a, hipStream_t s) {
   const long max_len = (long)a.max_pages * a.page_size;
-  Plan plan{0, gts_of(a.group), FastDiv((uint32_t)a.page_size)};
+  Plan plan{0, gts_of(a.group), FastDiv((uint32_t)a.page_size), 0, 1};
   if (!splits(a.n_seqs, a.kv_heads, a.group, max_len)) {
-    hipLaunchKernelGGL((paged_whole_kernel<F32, HELD, DH, ALIGNED>), dim3((unsigned)(a.n_seqs * a.kv_heads * plan.gts)),
+    hipLaunchKernelGGL((paged_whole_kernel<F32, E4M3, DH, ALIGNED>), dim3((unsigned)(a.n_seqs * a.kv_heads * plan.gts)),
                        dim3(kWholeWaves * 64), 0, s, a, plan);
     return hipGetLastError();
   }
   plan.wgs = workgroups(a.n_seqs, a.kv_heads, a.group, max_len);
-  hipLaunchKernelGGL((paged_split_kernel<F32, HELD, DH, ALIGNED>), dim3(plan.wgs), dim3(kSplitWaves * 64), 0, s, a, plan);
+  hipLaunchKernelGGL((paged_split_kernel<F32, E4M3, DH, ALIGNED>), dim3(plan.wgs), dim3(kSplitWaves * 64), 0, s, a, plan);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL((paged_join_kernel<F32, DH>), dim3(plan.wgs, std::min(a.group, kRows)), dim3(kJoinThreads), 0, s, a, plan);
@@ -673,27 +418,29 @@ hipError_t launch(const PagedArgs& a, hipStream_t s) {
 }
 
 template <bool F32, int DH>
-hipError_t launch_held(const PagedArgs& a, Held held, hipStream_t s) {
+hipError_t launch_held(const PagedArgs& a, bool e4m3, hipStream_t s) {
   // a block of 32 rows lies in one page where the page size is a multiple of 32
-  const bool whole = a.page_size % 32 == 0;
-  if (held == kE2M1) return whole ? launch<F32, kE2M1, DH, true>(a, s) : launch<F32, kE2M1, DH, false>(a, s);
-  if (held == kE4M3) return whole ? launch<F32, kE4M3, DH, true>(a, s) : launch<F32, kE4M3, DH, false>(a, s);
-  return whole ? launch<F32, kOwn, DH, true>(a, s) : launch<F32, kOwn, DH, false>(a, s);
+  if (a.page_size % 32 == 0) return e4m3 ? launch<F32, true, DH, true>(a, s) : launch<F32, false, DH, true>(a, s);
+  return e4m3 ? launch<F32, true, DH, false>(a, s) : launch<F32, false, DH, false>(a, s);
 }
 
 }  // namespace
 
 // Asked for as if every item were dealt from kLeastWhole rows on, so that a workspace
-// made for n_seqs and max_len serves fewer sequences too.
-size_t paged_attention_bytes(int n_seqs, int kv_heads, int group, int head_dim, long max_len) {
+// made for n_seqs and max_len serves fewer sequences too; over e2m1 rows as if items were taken four abreast.
+size_t paged_attention_bytes(int n_seqs, int kv_heads, int group, int head_dim, long max_len, bool e2m1) {
   if (n_seqs <= 0 || max_len <= kLeastWhole) return 0;
-  return (size_t)workgroups(n_seqs, kv_heads, group, max_len) * (2 * kRows * (head_dim + 2) * sizeof(float) + sizeof(Note));
+  const long tiles = (long)n_seqs * kv_heads * gts_of(group) * ((max_len + kTile - 1) / kTile);
+  const long runs = e2m1 ? std::min((long)kMostRuns, tiles) : workgroups(n_seqs, kv_heads, group, max_len);
+  return (size_t)runs * (2 * kRows * (head_dim + 2) * sizeof(float) + sizeof(Note));
 }
 
 hipError_t launch_paged_attention(const PagedArgs& a, bool bf16, Held held, int head_dim, hipStream_t s) {
   if (a.n_seqs <= 0) return hipSuccess;
-  if (bf16) return head_dim == 64 ? launch_held<false, 64>(a, held, s) : launch_held<false, 128>(a, held, s);
-  return head_dim == 64 ? launch_held<true, 64>(a, held, s) : launch_held<true, 128>(a, held, s);
+  if (held == kE2M1) return launch_paged_attention_e2m1(a, bf16, head_dim, s);
+  const bool e4m3 = held == kE4M3;
+  if (bf16) return head_dim == 64 ? launch_held<false, 64>(a, e4m3, s) : launch_held<false, 128>(a, e4m3, s);
+  return head_dim == 64 ? launch_held<true, 64>(a, e4m3, s) : launch_held<true, 128>(a, e4m3, s);
 }
 
 }  // namespace hsa

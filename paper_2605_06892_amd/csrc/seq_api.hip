@@ -202,7 +202,8 @@ HSA_API size_t hsa_paged_attention_workspace_bytes(int dtype, int32_t n_seqs, in
   if (!elem_size(dtype) || !heads_ok(heads, kv_heads, head_dim) || n_seqs < 0 || max_len < 0 ||
       max_len > kMaxKeys || n_seqs > kMaxRows / heads)
     return 0;
-  return hsa::paged_attention_bytes(n_seqs, kv_heads, heads / kv_heads, head_dim, max_len);
+  // for any cache: e2m1 rows take the most
+  return hsa::paged_attention_bytes(n_seqs, kv_heads, heads / kv_heads, head_dim, max_len, true);
 }
 
 HSA_API int hsa_paged_attention(int dtype, const void* q, int64_t q_stride, int cache_dtype,
@@ -230,8 +231,8 @@ HSA_API int hsa_paged_attention(int dtype, const void* q, int64_t q_stride, int 
   if (!rows_ok(q, n_seqs, q_stride, d, es) || !aligned(k_cache, row.align) || !aligned(v_cache, row.align) ||
       !aligned(o, es == 2 ? 16 : 4) || !aligned(lse, 4) || !aligned(page_table, 4) || !aligned(kv_lens, 4))
     return HSA_STEP_ERR_SHAPE;
-  const size_t need = hsa_paged_attention_workspace_bytes(dtype, n_seqs, heads, kv_heads, head_dim,
-                                                          (int64_t)max_pages * page_size);
+  const size_t need = hsa::paged_attention_bytes(n_seqs, kv_heads, heads / kv_heads, head_dim, (long)max_pages * page_size,
+                                                 row.held == hsa::kE2M1);
   if (need && (!workspace || workspace_bytes < need)) return HSA_STEP_ERR_WORKSPACE;
   if (need && !aligned(workspace, 16)) return HSA_STEP_ERR_SHAPE;
   const size_t cb = (size_t)n_rows * row.bytes, eb = (size_t)n_rows * row.exps;

@@ -24,6 +24,36 @@ constexpr int kExp4Min = -125, kExp4Max = 125, kExp4Nan = -128;
 // 2^e for -126 <= e <= 127
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(e + 127) << 23); }
 
+// 8 e2m1 codes of a word as bf16, times a power of two: exact
+__device__ __forceinline__ bf16x8 widen4(unsigned c, float scale) {
+  const bf16x2 p = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0), q = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1);
+  const bf16x2 r = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2), t = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3);
+  return (bf16x8){p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
+}
+
+// 8 fp32 values as three bf16 parts each, cut from the top: 8 + 8 + 8 bits, all that they have, but
+// for what lies under bf16's least value, 2^-133. What is not finite is its first part alone.
+__device__ __forceinline__ void cut3(const float (&x)[8], bf16x8 (&part)[3]) {
+  unsigned h[8], m[8], l[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const unsigned u = __float_as_uint(x[j]), mag = u & 0x7fffffffu;
+    h[j] = (u & 0xffff0000u) | (mag > 0x7f800000u ? 0x00400000u : 0u);  // a NaN whose upper bits say infinity
+    const float r = mag < 0x7f800000u ? x[j] - __uint_as_float(h[j]) : 0.f;
+    m[j] = __float_as_uint(r);
+    l[j] = __float_as_uint(r - __uint_as_float(m[j] & 0xffff0000u));
+  }
+  u32x4 p[3];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {  // the upper halves of two
+    p[0][j] = __builtin_amdgcn_perm(h[2 * j + 1], h[2 * j], 0x07060302);
+    p[1][j] = __builtin_amdgcn_perm(m[2 * j + 1], m[2 * j], 0x07060302);
+    p[2][j] = __builtin_amdgcn_perm(l[2 * j + 1], l[2 * j], 0x07060302);
+  }
+#pragma unroll
+  for (int i = 0; i < 3; ++i) part[i] = __builtin_bit_cast(bf16x8, p[i]);
+}
+
 // x / d for 0 <= x < 2^31 by a multiplication: with s = ceil(log2 d) and m =
 // floor(2^32 (2^s - d) / d) + 1 the quotient is (mulhi(x, m) + x) >> s.
 struct FastDiv {
@@ -86,8 +116,8 @@ struct PagedArgs {
   float* lse;
   void* ws;
 };
-// Workspace bytes of a launch, 0 where no sequence can be split.
-size_t paged_attention_bytes(int n_seqs, int kv_heads, int group, int head_dim, long max_len);
+// Workspace bytes of a launch, 0 where no sequence can be split; more over e2m1 rows.
+size_t paged_attention_bytes(int n_seqs, int kv_heads, int group, int head_dim, long max_len, bool e2m1);
 hipError_t launch_paged_attention(const PagedArgs& a, bool bf16, Held held, int head_dim, hipStream_t s);
 
 // Rows times weights in e2m1 groups (linear_w4.hip):
