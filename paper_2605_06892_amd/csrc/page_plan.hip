@@ -7,7 +7,9 @@
 // kChunk at a time, and writes what belongs to its own tokens: a token's sequence is found by a
 // search in the sums, its page is an old entry of the table or the ring's, and the token
 // that is the first of a new page writes it to the table. No workgroup waits for another.
-// Writing is all there is to it: 8 bytes per token; up to some 10^5 tokens the launch bounds it.
+// Writing is all there is to it, 8 bytes per token; what takes the time is a chain of reads: lengths, the sums and the
+// search in LDS, a page's number. A thousand prompts of 264 thousand tokens: 6.5 us with a token per thread, 9.2 with
+// four in turn, 8 with four at once; 48 sequences of one token 4.6-5.3.
 #include "seq_common.h"
 
 namespace hsa {
@@ -16,7 +18,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kPer = 4;                   // sequences per thread
 constexpr int kChunk = kThreads * kPer;   // sequences at a time
-constexpr int kTile = 1024;               // tokens at a time
+constexpr int kTile = kThreads;           // tokens at a time
+typedef int i32x4u __attribute__((ext_vector_type(4), aligned(4)));
 
 struct Lengths {
   int past, rows, have;  // rows before, all rows (at most the table's), pages before
@@ -25,20 +28,27 @@ struct Lengths {
 // x + y, at most `most`: for terms of 0 to `most` < 2^30 an associative sum that cannot wrap
 __device__ __forceinline__ int add_to(int x, int y, int most) { return min(x + y, most); }
 
+// x of the lane that CTRL says, 0 where there is none and in the rows of 16 that ROWS leaves out
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int from_lane(int x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, true);
+}
+
 // Exclusive sums of each thread's kPer values over the workgroup after `base`, at most `most`; returns the whole sum.
 __device__ __forceinline__ int exclusive(int (&v)[kPer], int base, int most, int* waves) {
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   int own = 0;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) own = add_to(own, v[i], most);
+  // over 16 lanes, then the last of 16 to the next 16, of 32 to the next 32
   int sum = own;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int y = __shfl_up(sum, o);
-    if (lane >= o) sum = add_to(sum, y, most);
-  }
-  int before = __shfl_up(sum, 1);
-  if (lane == 0) before = 0;
+  sum = add_to(sum, from_lane<0x111, 0xf>(sum), most);
+  sum = add_to(sum, from_lane<0x112, 0xf>(sum), most);
+  sum = add_to(sum, from_lane<0x114, 0xf>(sum), most);
+  sum = add_to(sum, from_lane<0x118, 0xf>(sum), most);
+  sum = add_to(sum, from_lane<0x142, 0xa>(sum), most);
+  sum = add_to(sum, from_lane<0x143, 0xc>(sum), most);
+  int before = from_lane<0x138, 0xf>(sum);  // the lane before
   __syncthreads();  // the last sums were read
   if (lane == kWave - 1) waves[wave] = sum;
   __syncthreads();
@@ -74,12 +84,20 @@ __global__ __launch_bounds__(kThreads) void page_plan_kernel(PagePlan a, FastDiv
   for (long s0 = 0; s0 < a.n_seqs; s0 += kChunk) {
     const int n = (int)min((long)kChunk, a.n_seqs - s0);
     int at[kPer], fresh[kPer], past[kPer], need[kPer];
+    const int j0 = threadIdx.x * kPer;
+    i32x4u fs = {}, ps = {};
+    if (j0 + kPer <= n) {
+      fs = *reinterpret_cast<const i32x4u*>(a.fresh + s0 + j0);
+      ps = *reinterpret_cast<const i32x4u*>(a.past + s0 + j0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (j0 + i < n) fs[i] = a.fresh[s0 + j0 + i], ps[i] = a.past[s0 + j0 + i];
+    }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int j = threadIdx.x * kPer + i;
-      fresh[i] = j < n ? min(max(a.fresh[s0 + j], 0), most) : 0;
-      past[i] = j < n ? min(max(a.past[s0 + j], 0), rows_most) : 0;
-      at[i] = fresh[i];
+      at[i] = fresh[i] = min(max(fs[i], 0), most);
+      past[i] = min(max(ps[i], 0), rows_most);
     }
     const int tokens_end = exclusive(at, tokens, most, waves);
 #pragma unroll
@@ -100,34 +118,31 @@ __global__ __launch_bounds__(kThreads) void page_plan_kernel(PagePlan a, FastDiv
     for (int i = 0; i < kPer; ++i) news[threadIdx.x * kPer + i] = need[i];
     if (threadIdx.x == 0) begins[kChunk] = tokens_end;
     __syncthreads();
+    int top = 1;  // the greatest power of two below the number of sequences
+    while (top * 2 < n) top *= 2;
     for (long t0 = ((long)(tokens / kTile - (int)blockIdx.x + (int)gridDim.x - 1) / (int)gridDim.x * (int)gridDim.x + (int)blockIdx.x) * kTile;
          t0 < tokens_end; t0 += (long)gridDim.x * kTile) {
-      for (int t = max((int)t0, tokens) + threadIdx.x; t < min(t0 + kTile, (long)tokens_end); t += kThreads) {
-        int lo = 0, hi = n;  // the last sequence that begins at t or before
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (begins[mid] <= t) lo = mid; else hi = mid;
-        }
-        const int pos = pasts[lo] + (t - begins[lo]);
-        int slot = -1;
-        if (pos < rows_most) {
-          const int rank = (int)page.quot(pos), in = pos - rank * a.page_size;
-          const int have = (int)page.quot(pasts[lo] + a.page_size - 1);
-          int32_t* entry = a.page_table + (s0 + lo) * (long)a.max_pages + rank;
-          int number;
-          if (rank < have) {
-            number = *entry;
-          } else {
-            const int j = news[lo] + rank - have;
-            number = j < ring.count ? a.free_pages[ring.first + (long)j >= a.n_free ? ring.first + (long)j - a.n_free : ring.first + j] : -1;
-            if (in == 0) *entry = number;
-          }
-          const long row = (long)number * a.page_size + in;
-          slot = number < 0 || row > INT32_MAX ? -1 : (int)row;
-        }
-        a.pos[t] = pos;
-        a.slots[t] = slot;
+      const int t = (int)t0 + (int)threadIdx.x;
+      if (t < tokens || t >= tokens_end) continue;
+      int seq = 0;  // the last sequence that begins at t or before
+      for (int step = top; step > 0; step >>= 1)
+        if (seq + step < n && begins[seq + step] <= t) seq += step;
+      const int past = pasts[seq], pos = past + (t - begins[seq]);
+      int slot = -1;
+      if (pos < rows_most) {
+        const int rank = (int)page.quot(pos), in = pos - rank * a.page_size, have = (int)page.quot(past + a.page_size - 1);
+        const int j = news[seq] + rank - have;
+        int32_t* entry = a.page_table + (s0 + seq) * (long)a.max_pages + rank;
+        // the page's number: an old entry of the table, or the ring's
+        const long k = ring.first + (long)j;
+        const int32_t* from = rank < have ? entry : a.free_pages + (k >= a.n_free ? k - a.n_free : k);
+        const int number = rank < have || j < ring.count ? *from : -1;
+        if (rank >= have && in == 0) *entry = number;  // a new page's first token
+        const long row = (long)number * a.page_size + in;
+        slot = number < 0 || row > INT32_MAX ? -1 : (int)row;
       }
+      a.pos[t] = pos;
+      a.slots[t] = slot;
     }
     __syncthreads();  // the sums were read
     tokens = tokens_end;
