@@ -193,6 +193,38 @@ def test_linear(dtype, out, rows, d_in, d_out):
     y.check("y")
 
 
+# every shape of launch: the outputs that ask for 1, 2, 4 and 8 waves beside each other, one and more tiles of rows, splits
+# that end inside a unit of 512 inputs, and products shorter than one
+SHAPES = [(r, k, n) for n in (200, 4100, 8200) for r, k in ((1, 544), (5, 4640), (16, 1056), (17, 2080), (33, 544), (64, 96))] + \
+    [(21, 96, 16400), (11, 608, 16400), (3, 1120, 16400), (32, 608, 32800), (64, 544, 32800), (33, 64, 32800)]
+
+
+@pytest.mark.parametrize("rows,d_in,d_out", SHAPES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linear_every_launch(dtype, rows, d_in, d_out):
+    x, codes, ex = linear_case(rows + d_out, dtype, rows, d_in, d_out)
+    y = Guarded((rows, d_out), T[dtype], 1)
+    H.hsa_linear_w4(x.to(DEV), rows, codes.to(DEV), ex.to(DEV), y.t)
+    linear_check(y.t, x, codes, ex, dtype)
+    y.check("y")
+
+
+@pytest.mark.parametrize("scale", [-100, -115, -126])
+def test_linear_small_f32_rows(scale):
+    """fp32 rows are taken to within 2^-133 of each value: with values about 2^-115 that shows in an output of ordinary size."""
+    g = S._gen(8)
+    x = S._randn(g, 3, 640) * 2.0 ** scale
+    codes = torch.randint(0, 256, (70, 320), generator=g).to(torch.uint8)
+    ex = torch.randint(100, 111, (70, 20), generator=g).to(torch.int8)
+    y = torch.empty(3, 70, device=DEV)
+    H.hsa_linear_w4(x.to(DEV), 3, codes.to(DEV), ex.to(DEV), y)
+    w = values4(codes, ex)
+    want, A = x.double() @ w.t(), x.double().abs() @ w.abs().t()
+    bar = 2 * (640 + 16) * U * A + 2.0 ** -133 * w.abs().sum(1) + 1e-37
+    off = (y.cpu().double() - want).abs()
+    assert torch.all(off <= bar), f"{float((off / bar).max()):.2f} of the bound"
+
+
 @pytest.mark.parametrize("rows,d_in,d_out", [(1, 64, 7), (9, 1056, 130), (40, 288, 65), (2, 2048, 600)])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("what", ["scale", "gelu", "scale+gelu", "residual", "scale+residual", "in place", "scale f32"])
@@ -358,6 +390,68 @@ def test_paged(dtype, wide, dh, lens, page, heads, kv):
     S.check(o.t, lse, want, lw, A, Sm, dtype, max(lens), dh)
     o.check("o")
     ws.check("workspace")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,page,heads,kv,rows", [
+    ([2000, 900, 0, 1], 32, 140, 140, 2016),    # more items than runs go round: the tiles of all in one order
+    ([1500, 3], 16, 300, 300, 1504),
+    ([3000, 70, 1111], 64, 68, 4, 4096),        # groups of 17: two items of one head beside each other
+    ([3000, 70, 1111], 20, 34, 2, 4000),
+    ([5000], 64, 24, 8, 8192),
+    ([4097, 4096], 32, 6, 6, 4128),
+    ([9, 300, 700, 1, 0] * 32, 32, 16, 8, 704),   # short ones, four items to a workgroup
+    ([9, 300, 700, 1, 0] * 32, 20, 34, 2, 760),
+    ([33, 64, 500] * 100, 64, 6, 6, 512),
+], ids=range(9))
+def test_paged_every_launch(dtype, lens, page, heads, kv, rows):
+    dh = 64
+    q, k, v, held, table = paged_inputs4(len(lens), dtype, lens, page, heads, kv, dh, max_pages=rows // page)
+    nb = H.hsa_paged_attention_workspace_bytes(T[dtype], len(lens), heads, kv, dh, table.shape[1] * page)
+    o, ws = Guarded(q.shape, T[dtype], 1), Guarded((max(nb, 1),), torch.uint8, 2)
+    ws.t.fill_(255)
+    _, lse = S.run_paged(q, held, table, lens, page, heads, kv, dh, 0.125, o.t, ws.t)
+    want, lw, A, Sm = S.paged_want(q, k, v, table, lens, page, k.shape[0] // page, heads, kv, dh, 0.125)
+    S.check(o.t, lse, want, lw, A, Sm, dtype, max(lens), dh)
+    o.check("o")
+    ws.check("workspace")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("max_pages", [0, 3, 300])
+def test_paged_without_rows(dtype, max_pages):
+    """No pages in the table, and no pages in the cache: outputs of zeros."""
+    q = torch.ones(2, 256, dtype=T[dtype])
+    c, e = torch.empty(0, 64, dtype=torch.uint8), torch.empty(0, 4, dtype=torch.int8)
+    table = torch.zeros(2, max_pages, dtype=torch.int32)
+    o, lse = S.run_paged(q, (c, c, e, e), table, [5, 0], 16, 2, 1, 128, 0.1)
+    assert torch.all(o == 0) and torch.all(lse == -math.inf)
+
+
+@pytest.mark.parametrize("page", [32, 24])
+def test_paged_length_at_the_limit(page):
+    """The longest length the call takes, all its pages the same two; its waves add up 2^19 weights in each lane at most."""
+    q, k, v, held, table = paged_inputs4(31, "bf16", [2 * page], page, 2, 1, 64, spare=0)
+    pages = 2 ** 30 // page
+    n = pages * page
+    table = torch.full((1, pages), int(table[0, 1]), dtype=torch.int32).index_fill(1, torch.tensor([0]), int(table[0, 0]))
+    o, lse = S.run_paged(q, held, table, [n], page, 2, 1, 64, 0.125)
+    first, rest = int(table[0, 0]) * page, int(table[0, 1]) * page
+    for h in range(2):
+        s = [(k[r:r + page].double() @ q[0, h * 64:h * 64 + 64].double()) * 0.125 for r in (first, rest)]
+        w = torch.cat([s[0], s[1] + math.log(pages - 1)])
+        want = torch.softmax(w, 0) @ torch.cat([v[first:first + page], v[rest:rest + page]]).double()
+        assert float((o[0, h * 64:h * 64 + 64].cpu().double() - want).abs().max()) < (2.0 ** -7 + 2 ** 20 * U) * float(v.abs().max())
+        assert abs(float(lse[0, h]) - float(torch.logsumexp(w, 0))) < 2 ** 19 * U + 1e-5
+
+
+def test_paged_f32_large_scores():
+    """Scores of some thousands in fp32, where one that is off by bf16's step would choose other rows."""
+    q, k, v, held, table = paged_inputs4(3, "f32", [300, 77], 16, 4, 2, 64)
+    q = q * 300
+    o, lse = S.run_paged(q, held, table, [300, 77], 16, 4, 2, 64, 0.125)
+    want, lw, A, Sm = S.paged_want(q, k, v, table, [300, 77], 16, k.shape[0] // 16, 4, 2, 64, 0.125)
+    S.check(o, lse, want, lw, A, Sm, "f32", 300, 64)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

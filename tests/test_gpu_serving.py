@@ -54,7 +54,8 @@ def norm_check(got, want, bar, dtype):
     assert torch.all(off <= bar), f"{float((off / bar).max()):.2f} of the bound"
 
 
-@pytest.mark.parametrize("n,heads,kv", [(1, 1, 1), (1, 40, 8), (5, 3, 2), (16, 16, 2), (133, 5, 5), (700, 12, 4)])
+@pytest.mark.parametrize("n,heads,kv", [(1, 1, 1), (1, 40, 8), (5, 3, 2), (16, 16, 2), (133, 5, 5), (700, 12, 4),
+                                        (1501, 40, 7)])  # the last: launches of two heads to a thread, an odd number of them
 @pytest.mark.parametrize("dh", [64, 128])
 @pytest.mark.parametrize("rope_dim", [0, 8, 24, 64, 128])
 @pytest.mark.parametrize("interleaved", [False, True])
