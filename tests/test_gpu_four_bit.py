@@ -394,15 +394,15 @@ def test_paged(dtype, wide, dh, lens, page, heads, kv):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("lens,page,heads,kv,rows", [
-    ([2000, 900, 0, 1], 32, 140, 140, 2016),    # more items than runs go round: the tiles of all in one order
-    ([1500, 3], 16, 300, 300, 1504),
+    ([900, 70, 0, 1], 32, 140, 140, 2112),      # more items than runs go round: the tiles of all in one order
+    ([300, 3], 16, 300, 300, 2064),
     ([3000, 70, 1111], 64, 68, 4, 4096),        # groups of 17: two items of one head beside each other
     ([3000, 70, 1111], 20, 34, 2, 4000),
     ([5000], 64, 24, 8, 8192),
     ([4097, 4096], 32, 6, 6, 4128),
     ([9, 300, 700, 1, 0] * 32, 32, 16, 8, 704),   # short ones, four items to a workgroup
     ([9, 300, 700, 1, 0] * 32, 20, 34, 2, 760),
-    ([33, 64, 500] * 100, 64, 6, 6, 512),
+    ([33, 64, 500] * 60, 64, 6, 6, 512),
 ], ids=range(9))
 def test_paged_every_launch(dtype, lens, page, heads, kv, rows):
     dh = 64
