@@ -14,7 +14,7 @@
 // product is exact here too, and sums are in fp32 as before (what of a value lies under 2^-133, bf16's least, is
 // left out). The parts are columns of their own, five rows to a tile, summed at the end. The fp32
 // matrix instructions are 16 times slower than the bf16 ones: 5 rows of 8960 by 1537 outputs take 16 us with them,
-// 12 so, of 8192 by 16384 48 and 21.
+// 11 so, of 8192 by 16384 48 and 21.
 //
 // One row of 8192 by 32768 outputs: 30 us, 4.7 TB/s; 16 rows 37 us.
 #include "seq_common.h"
@@ -53,9 +53,10 @@ __global__ __launch_bounds__(kMostWaves * kWave) void linear_w4_kernel(LinearW4 
   const uint8_t* w = a.w + w_row * (a.d_in / 2);
   const int8_t* exps = a.exps + w_row * groups;
 
-  // x of a unit in LDS, two units of each split: row r at r * 1 KB, its 16-byte chunk c at c ^ (r & 7), so that
+  // x of a unit in LDS, two units of each split (one where a wave reads what it wrote itself): row r at r * 1 KB, its 16-byte chunk c at c ^ (r & 7), so that
   // 8 rows' reads of one chunk spread over the banks. Rows past the last repeat it.
-  char* xl = lds + ks * 2 * x_rows * 1024;
+  const int bufs = outs > 1 ? 2 : 1;
+  char* xl = lds + ks * bufs * x_rows * 1024;
   u32x4 xr[XS][XL];
   auto load_x = [&](int u) {
     const int k = min(u * kUnit + lane * 8, a.d_in - 8);
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(kMostWaves * kWave) void linear_w4_kernel(LinearW4 
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    buf ^= 1;
+    buf ^= bufs - 1;
     if constexpr (more) {
       stage(buf);
       e = e_next;
@@ -206,7 +207,7 @@ template <bool BF16, int NT, int XS>
 hipError_t launch(const LinearW4& a, int outs, int splits, hipStream_t s) {
   constexpr int ROWS = NT * (BF16 ? kOuts : 5);
   const unsigned wgs = (unsigned)((a.d_out + outs * kOuts - 1) / (outs * kOuts)), tiles = (unsigned)((a.rows + ROWS - 1) / ROWS);
-  const int lds = std::max(splits * 2 * XS * outs * (BF16 ? 1 : 3), outs * splits * NT) * 1024;
+  const int lds = std::max(splits * (outs > 1 ? 2 : 1) * XS * outs * (BF16 ? 1 : 3), outs * splits * NT) * 1024;
   hipLaunchKernelGGL((linear_w4_kernel<BF16, NT, XS>), dim3(wgs, tiles), dim3(outs * splits * kWave), lds, s, a, outs, splits);
   return hipGetLastError();
 }
@@ -233,7 +234,8 @@ hipError_t launch_f32(const LinearW4& a, int outs, int splits, hipStream_t s) {
 }  // namespace
 
 // Tiles of rows, waves that share inputs and waves that share outputs: as many of the former as leave a workgroup
-// for each CU, for they share what is read of x, and the latter where there is enough to split. us:
+// for each CU, for they share what is read of x, and the latter where there is enough to split (6 of 5 fp32 rows, 8960 by 1537
+// outputs: 10.9 us, 12.4 with 4; in bf16 6 are no faster). us:
 //                          1x4  2x2  4x1  4x2  8x1             2 tiles 4x1  8x1   4 tiles 8x1
 //    4 rows, 8960 x 1536   6.6  8.5 12.7 12.6 22.5
 //    4       5120 x 5120   9.2  7.4 10.9 10.3 18.2
@@ -248,7 +250,7 @@ hipError_t launch_linear_w4(const LinearW4& a, bool bf16, hipStream_t s) {
   const long outs = (a.d_out + kOuts - 1) / kOuts, cus = compute_units();
   const int units = (a.d_in + kUnit - 1) / kUnit;
   const bool many = outs >= 2 * cus, some = outs >= cus;
-  const int four = units >= 8 ? 2 : 1, two = units >= 2 ? 2 : 1, one = std::min(units, 4);  // splits beside 4, 2 and 1
+  const int four = units >= 8 ? 2 : 1, two = units >= 2 ? 2 : 1, one = std::min(units, bf16 || a.rows > 5 ? 4 : 6);  // splits beside 4, 2 and 1
   if (!bf16) {
     if (a.rows > 10 && outs >= 4 * cus) return launch_f32<4>(a, 4, 1, s);
     if (many || (some && a.rows > 5)) return launch_f32<1>(a, 4, four, s);
