@@ -655,8 +655,9 @@ int hsa_packed_attention(int dtype, const void* q, int64_t q_stride, const void*
 #define HSA_STEP_PAGED_WORKSPACE_BYTES (32u << 20)
 
 /* Workspace bytes hsa_paged_attention needs, at most
- * HSA_STEP_PAGED_WORKSPACE_BYTES, and enough for fewer sequences and rows too. 0 where
- * it needs none, and for invalid sizes. */
+ * HSA_STEP_PAGED_WORKSPACE_BYTES, and enough for fewer sequences and rows too, and for every
+ * cache_dtype (HSA_STEP_E2M1 takes the most, up to twice the others). 0 where it needs none, and
+ * for invalid sizes. */
 size_t hsa_paged_attention_workspace_bytes(int dtype, int32_t n_seqs, int32_t heads,
                                            int32_t kv_heads, int32_t head_dim, int64_t max_len);
 
@@ -675,7 +676,7 @@ size_t hsa_paged_attention_workspace_bytes(int dtype, int32_t n_seqs, int32_t he
  * sequence's length are not read. Rows of the caches that no sequence has may
  * hold anything, exponents that were never written among it.
  *   q            [n_seqs, heads * head_dim] dtype, rows q_stride elements apart
- *   k_cache, ... as for hsa_cache_store, with n_pages * page_size rows
+ *   k_cache, ... as for hsa_cache_store, with n_pages * page_size rows, of any cache_dtype
  *   page_table   int32 [n_seqs, max_pages]; pages may be shared by sequences
  *   kv_lens      int32 [n_seqs] on the device, clamped to [0, max_pages * page_size]
  *   scale        > 0, at most 2^127
@@ -719,8 +720,8 @@ int hsa_quantize_w4(int dtype, const void* w, int64_t w_stride, int64_t n_rows, 
  *              y otherwise
  *   y          [n_rows, d_out] out_dtype
  * out_dtype is dtype, or HSA_STEP_F32 with dtype HSA_STEP_BF16 (then no residual and no
- * GELU); GELU takes no residual. d_in is a multiple of 32; d_in, d_out and n_rows are at most
- * 2^22; x, w, residual and y are 16-byte aligned. y must not overlap x, w, w_exp or row_scale.
+ * GELU); GELU takes no residual. d_in is a multiple of 32; d_in and d_out are at most 2^22,
+ * n_rows 2^18; x, w, residual and y are 16-byte aligned. y must not overlap x, w, w_exp or row_scale.
  */
 int hsa_linear_w4(int dtype, const void* x, int32_t n_rows, int32_t d_in, const void* w,
                   const int8_t* w_exp, int32_t d_out, const float* row_scale, const void* residual,

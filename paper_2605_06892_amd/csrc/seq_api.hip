@@ -10,6 +10,7 @@ namespace {
 constexpr int64_t kMaxStride = int64_t(1) << 22;  // elements between rows
 constexpr int64_t kMaxKeys = int64_t(1) << 30;    // keys of a sequence, so that a position plus a block fits an int
 constexpr int64_t kMaxLaunch = int64_t(1) << 32;  // threads of one launch
+constexpr int64_t kMaxW4Rows = int64_t(1) << 18;  // fewer than 2^16 tiles of 5 rows, a launch's second dimension
 
 // Bytes from the first to the end of the last of n rows `stride` elements apart.
 size_t span(int64_t n, int64_t stride, int64_t width, size_t es) {
@@ -283,7 +284,7 @@ HSA_API int hsa_linear_w4(int dtype, const void* x, int32_t n_rows, int32_t d_in
   const size_t es = elem_size(dtype), os = elem_size(out_dtype);
   if (!es || (out_dtype != dtype && !(dtype == HSA_STEP_BF16 && out_dtype == HSA_STEP_F32))) return HSA_STEP_ERR_DTYPE;
   if (n_rows < 0 || d_in < 1 || d_in > kMaxStride || d_in % hsa::kGroup != 0 || d_out < 0 || d_out > kMaxStride ||
-      n_rows > kMaxStride)
+      n_rows > kMaxW4Rows)
     return HSA_STEP_ERR_SHAPE;
   if ((gelu && residual) || (out_dtype != dtype && (gelu || residual))) return HSA_STEP_ERR_SHAPE;
   if (n_rows == 0 || d_out == 0) return HSA_STEP_OK;

@@ -304,6 +304,19 @@ def test_linear_offsets_past_32_bits(d_in, d_out):
     assert torch.equal(y.view(2, -1, 1000), y[:, :1000][:, None].expand(2, d_out // 1000, 1000))
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_linear_as_many_rows_as_it_takes(dtype):
+    """2^18 rows: the tiles of rows fit the launch. All rows the same but for a factor that is exact."""
+    x, codes, ex = linear_case(9, dtype, 4, 32, 3)
+    n = 2 ** 18
+    rows = x.to(DEV).repeat(n // 4, 1)
+    rows[n // 2:] *= 4
+    y = torch.empty(n, 3, dtype=T[dtype], device=DEV)
+    H.hsa_linear_w4(rows, n, codes.to(DEV), ex.to(DEV), y)
+    linear_check(y[:4], x, codes, ex, dtype)
+    assert torch.equal(y[:n // 2].view(-1, 4, 3), y[:4].expand(n // 8, 4, 3)) and torch.equal(y[n // 2:], 4 * y[:n // 2])
+
+
 def test_linear_other_stream_and_graph():
     x, codes, ex = (t.to(DEV) for t in linear_case(6, "bf16", 3, 1024, 500))
     want, y = (torch.empty(3, 500, dtype=torch.bfloat16, device=DEV) for _ in range(2))

@@ -75,7 +75,7 @@ LINEAR = dict(dtype=BF16, x=P[0], n_rows=4, d_in=512, w=P[1], w_exp=P[2], d_out=
 
 @pytest.mark.parametrize("change,status", [
     (dict(dtype=E2M1), DTYPE), (dict(out_dtype=E4M3), DTYPE), (dict(dtype=F32), DTYPE), (dict(out_dtype=7), DTYPE),
-    (dict(n_rows=-1), SHAPE), (dict(n_rows=2 ** 22 + 1), SHAPE), (dict(d_in=0), SHAPE), (dict(d_in=40), SHAPE),
+    (dict(n_rows=-1), SHAPE), (dict(n_rows=2 ** 18 + 1), SHAPE), (dict(d_in=0), SHAPE), (dict(d_in=40), SHAPE),
     (dict(d_in=-32), SHAPE), (dict(d_in=2 ** 22 + 32), SHAPE), (dict(d_out=-1), SHAPE), (dict(d_out=2 ** 22 + 1), SHAPE),
     (dict(gelu=1), SHAPE), (dict(out_dtype=F32), SHAPE), (dict(out_dtype=F32, residual=None, gelu=1), SHAPE),
     (dict(x=P[0] + 8), SHAPE), (dict(w=P[1] + 8), SHAPE), (dict(y=P[5] + 4), SHAPE), (dict(residual=P[4] + 8), SHAPE),
