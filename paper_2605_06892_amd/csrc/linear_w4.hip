@@ -53,8 +53,8 @@ __global__ __launch_bounds__(kMostWaves * kWave) void linear_w4_kernel(LinearW4 
   const uint8_t* w = a.w + w_row * (a.d_in / 2);
   const int8_t* exps = a.exps + w_row * groups;
 
-  // x of a unit in LDS, two units of each split (one where a wave reads what it wrote itself): row r at r * 1 KB, its 16-byte chunk c at c ^ (r & 7), so that
-  // 8 rows' reads of one chunk spread over the banks. Rows past the last repeat it.
+  // x of a unit in LDS, two units of each split (one where a wave reads what it wrote itself): row r at r * 1 KB, its
+  // 16-byte chunk c at c ^ (r & 7), so that 8 rows' reads of one chunk spread over the banks. Rows past the last repeat it.
   const int bufs = outs > 1 ? 2 : 1;
   char* xl = lds + ks * bufs * x_rows * 1024;
   u32x4 xr[XS][XL];

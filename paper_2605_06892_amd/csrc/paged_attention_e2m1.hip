@@ -28,13 +28,8 @@ namespace {
 
 constexpr int kWaves = 8;
 
-// bf16 queries over e2m1 rows. What bounds the reading of so few bytes is how many loads there are and how many bytes
-// are under way, so a block of 32 keys is five loads (two of K, two of V, one of exponents: V's in the
-// lower lanes, K's in the upper), DEPTH blocks ahead. They do not depend on whether there is such a
-// block: where there is none they read the cache's first row, so that a wait for one block leaves the later ones
-// under way. K goes from its loads to the products: slot lane / 16 has a quarter of a head's channels, which share an
-// exponent. V's codes and all exponents go through LDS, where a lane reads DT neighbouring channels of its
-// slot's 8 keys and pairs keys in registers, as the products contract over them.
+// The loads of a block do not depend on whether there is such a block: where there is none they read the cache's first
+// row, so that a wait for one block leaves the later one under way.
 template <bool F32, int DH, bool ALIGNED>
 struct Attend {
   static constexpr int NW = kWaves, PARTS = F32 ? 3 : 1;  // waves; bf16 parts of a query and of a probability
