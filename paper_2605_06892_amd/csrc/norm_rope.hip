@@ -96,10 +96,13 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormRope a, FastDiv
     if (h < a.heads) Eight<BF16, NEAR, PAST>::load(a.q, row * a.q_stride + h * DH, c0, c1, x[u], y[u]);
     else if (h < a.heads + a.kv_heads) Eight<BF16, NEAR, PAST>::load(a.k, row * a.k_stride + (h - a.heads) * DH, c0, c1, x[u], y[u]);
   }
-  f32x4 cs[2] = {{1.f, 0.f, 1.f, 0.f}, {1.f, 0.f, 1.f, 0.f}};
+  // channels that are not turned are kept, not turned by 0: their pair may hold what is not finite
+  bool turn = false;
+  f32x4 cs[2] = {};
   if (pair < a.rope_dim / 2) {
     const long p = a.pos ? a.pos[row] : row;
-    if (p >= 0 && p < a.n_pos) {
+    turn = p >= 0 && p < a.n_pos;
+    if (turn) {
       const f32x4* t = reinterpret_cast<const f32x4*>(a.rope + p * a.rope_dim + pair * 2);
       cs[0] = t[0];
       cs[1] = t[1];
@@ -132,22 +135,21 @@ __global__ __launch_bounds__(kThreads) void norm_rope_kernel(NormRope a, FastDiv
     f32x4 wx = {1.f, 1.f, 1.f, 1.f}, wy = wx;
     if (weight) Eight<BF16, NEAR, PAST>::load(weight, 0, c0, c1, wx, wy);
     const f32x4 p = x[u] * g * wx, q = y[u] * g * wy;
-    f32x4 v, w;
-    if (a.interleaved) {
+    f32x4 v = p, w = q;
+    if (turn) {
+      if constexpr (NEAR) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const f32x2 r = rope_rotate((f32x2){cs[0][2 * j], cs[0][2 * j + 1]}, p[2 * j], p[2 * j + 1]);
-        const f32x2 t = rope_rotate((f32x2){cs[1][2 * j], cs[1][2 * j + 1]}, q[2 * j], q[2 * j + 1]);
-        v[2 * j] = r[0], v[2 * j + 1] = r[1], w[2 * j] = t[0], w[2 * j + 1] = t[1];
-      }
-    } else if constexpr (NEAR) {  // no rotation
-      v = p;
-      w = q;
-    } else {
+        for (int j = 0; j < 2; ++j) {
+          const f32x2 r = rope_rotate((f32x2){cs[0][2 * j], cs[0][2 * j + 1]}, p[2 * j], p[2 * j + 1]);
+          const f32x2 t = rope_rotate((f32x2){cs[1][2 * j], cs[1][2 * j + 1]}, q[2 * j], q[2 * j + 1]);
+          v[2 * j] = r[0], v[2 * j + 1] = r[1], w[2 * j] = t[0], w[2 * j + 1] = t[1];
+        }
+      } else {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const f32x2 r = rope_rotate((f32x2){cs[j >> 1][2 * (j & 1)], cs[j >> 1][2 * (j & 1) + 1]}, p[j], q[j]);
-        v[j] = r[0], w[j] = r[1];
+        for (int j = 0; j < 4; ++j) {
+          const f32x2 r = rope_rotate((f32x2){cs[j >> 1][2 * (j & 1)], cs[j >> 1][2 * (j & 1) + 1]}, p[j], q[j]);
+          v[j] = r[0], w[j] = r[1];
+        }
       }
     }
     if (is_q) Eight<BF16, NEAR, PAST>::store(a.q_out, row * a.qo_stride + h * DH, c0, c1, v, w);

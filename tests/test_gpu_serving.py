@@ -136,6 +136,32 @@ def test_norm_rope_at_the_limits(dtype, interleaved):
         assert torch.all(ko == 0)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("n", [4, 512])  # the latter in launches of two heads to a thread
+def test_norm_rope_keeps_what_is_not_finite_in_its_pair(dtype, interleaved, n):
+    """An infinite value makes its channel NaN, and its pair's where that is turned; all others of its head are 0."""
+    heads, dh, rope_dim = 64, 128, 64
+    x = S._randn(S._gen(3), n, heads, dh).to(T[dtype])
+    at = [(0, 2, 70), (0, 3, 127), (1, 0, 5), (2, 1, 9), (3, 63, 40)]
+    want = torch.zeros(n, heads, dh, dtype=torch.bool)
+    pos = torch.arange(n, dtype=torch.int32)
+    pos[2] = -1
+    for r, h, c in at:
+        x[r, h, c] = math.inf
+        want[r, h, c] = True
+        if c < rope_dim and r != 2:
+            want[r, h, c ^ 1 if interleaved else (c + rope_dim // 2) % rope_dim] = True
+    x = x.view(n, -1)
+    out = torch.empty(n, heads * dh, dtype=T[dtype], device=DEV)
+    H.hsa_qk_norm_rope(x.to(DEV), None, heads, 0, dh, out, None, rope=angles(n, rope_dim).to(DEV), pos=pos.to(DEV),
+                       interleaved=interleaved)
+    got = out.cpu().view(n, heads, dh)
+    assert torch.equal(got.isnan(), want)
+    for r, h, _ in at:
+        assert torch.all(got[r, h][~want[r, h]] == 0)
+
+
 def test_norm_rope_turns_as_the_stack_does():
     """A table of one row per token of a grid, the sum of its coordinates' rows of hsa_rope_table."""
     grid, dh, n = (3, 4, 5), 128, 60
