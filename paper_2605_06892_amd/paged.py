@@ -169,8 +169,10 @@ class Layer4:
 
     def step(self, x: torch.Tensor, c: PagedCache, pool: PagePool, rope: torch.Tensor | None, y: torch.Tensor,
              prompts: bool = False) -> None:
-        """y = the layer's output for the tokens x of pool.plan's last step: one for every sequence, or with
-        `prompts` any number, where sequences begin. y may be x."""
+        """y = the layer's output for the tokens x of pool.plan's last step: exactly one for every sequence, in their
+        order (fresh was 1 throughout; an ended sequence goes on with any token and is released when another
+        takes its place), or with `prompts` any number, where sequences begin (they attend to themselves
+        only). y may be x."""
         n = x.shape[0]
         q_width, kv_width = self.heads * self.head_dim, self.kv_heads * self.head_dim
         qkv, o = self.qkv[:n], self.o[:n]
