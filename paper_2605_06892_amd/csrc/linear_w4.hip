@@ -234,8 +234,10 @@ hipError_t launch_f32(const LinearW4& a, int outs, int splits, hipStream_t s) {
 }  // namespace
 
 // Tiles of rows, waves that share inputs and waves that share outputs: as many of the former as leave a workgroup
-// for each CU, for they share what is read of x, and the latter where there is enough to split (6 of 5 fp32 rows, 8960 by 1537
-// outputs: 10.9 us, 12.4 with 4; in bf16 6 are no faster). us:
+// for each CU, for they share what is read of x, and the latter where there is enough to split: waves that share nothing else
+// as many as up to 8 take the units in equally many turns, for what is left over is loaded without a turn before it. 5 fp32 rows,
+// 10 units: 5 splits 7.9 us, 4 8.9, 6 8.7, 8 9.1; 16 units: 8 8.5, 4 10.2, 6 10.8; 18: 6 10.9, 4 12.5, 8 11.4; 27: 7 15.3, 4 16.6,
+// 8 15.7; 4 bf16 rows, 7 units: 7 4.4, 4 5.0; 10: 5 5.1, 4 5.7; 18 and 32 within 2%. Waves x splits, us:
 //                          1x4  2x2  4x1  4x2  8x1             2 tiles 4x1  8x1   4 tiles 8x1
 //    4 rows, 8960 x 1536   6.6  8.5 12.7 12.6 22.5
 //    4       5120 x 5120   9.2  7.4 10.9 10.3 18.2
@@ -250,7 +252,7 @@ hipError_t launch_linear_w4(const LinearW4& a, bool bf16, hipStream_t s) {
   const long outs = (a.d_out + kOuts - 1) / kOuts, cus = compute_units();
   const int units = (a.d_in + kUnit - 1) / kUnit;
   const bool many = outs >= 2 * cus, some = outs >= cus;
-  const int four = units >= 8 ? 2 : 1, two = units >= 2 ? 2 : 1, one = std::min(units, bf16 || a.rows > 5 ? 4 : 6);  // splits beside 4, 2 and 1
+  const int four = units >= 8 ? 2 : 1, two = units >= 2 ? 2 : 1, turns = (units + 7) / 8, one = (units + turns - 1) / turns;  // splits beside 4, 2 and 1
   if (!bf16) {
     if (a.rows > 10 && outs >= 4 * cus) return launch_f32<4>(a, 4, 1, s);
     if (many || (some && a.rows > 5)) return launch_f32<1>(a, 4, four, s);

@@ -209,6 +209,18 @@ def test_linear_every_launch(dtype, rows, d_in, d_out):
     y.check("y")
 
 
+@pytest.mark.parametrize("units", [2, 3, 4, 5, 6, 7, 8, 9, 10, 11, 13, 16, 18, 25])
+@pytest.mark.parametrize("less", [0, 480])
+@pytest.mark.parametrize("dtype,rows", [("bf16", 3), ("bf16", 16), ("bf16", 20), ("f32", 1), ("f32", 5), ("f32", 9)])
+def test_linear_every_split(dtype, rows, units, less):
+    """Few outputs, whose inputs are taken by up to 8 waves in turns: full ones, and some of a last unit of one group."""
+    x, codes, ex = linear_case(units, dtype, rows, units * 512 - less, 100)
+    y = Guarded((rows, 100), T[dtype], 1)
+    H.hsa_linear_w4(x.to(DEV), rows, codes.to(DEV), ex.to(DEV), y.t)
+    linear_check(y.t, x, codes, ex, dtype)
+    y.check("y")
+
+
 @pytest.mark.parametrize("scale", [-100, -115, -126])
 def test_linear_small_f32_rows(scale):
     """fp32 rows are taken to within 2^-133 of each value: with values about 2^-115 that shows in an output of ordinary size."""
