@@ -35,13 +35,23 @@ __device__ __forceinline__ bf16x8 widen4(unsigned c, float scale) {
 // for what lies under bf16's least value, 2^-133. What is not finite is its first part alone.
 __device__ __forceinline__ void cut3(const float (&x)[8], bf16x8 (&part)[3]) {
   unsigned h[8], m[8], l[8];
+  float odd = 0.f;  // NaN if a value is not finite, for what is left of that then is
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const unsigned u = __float_as_uint(x[j]), mag = u & 0x7fffffffu;
-    h[j] = (u & 0xffff0000u) | (mag > 0x7f800000u ? 0x00400000u : 0u);  // a NaN whose upper bits say infinity
-    const float r = mag < 0x7f800000u ? x[j] - __uint_as_float(h[j]) : 0.f;
+    h[j] = __float_as_uint(x[j]);
+    const float r = x[j] - __uint_as_float(h[j] & 0xffff0000u);
     m[j] = __float_as_uint(r);
-    l[j] = __float_as_uint(r - __uint_as_float(m[j] & 0xffff0000u));
+    const float t = r - __uint_as_float(m[j] & 0xffff0000u);
+    l[j] = __float_as_uint(t);
+    odd += t;
+  }
+  if (__any(odd != odd)) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const unsigned mag = h[j] & 0x7fffffffu;
+      if (mag >= 0x7f800000u) m[j] = l[j] = 0;
+      if (mag > 0x7f800000u) h[j] |= 0x00400000u;  // a NaN whose upper bits say infinity
+    }
   }
   u32x4 p[3];
 #pragma unroll
