@@ -14,7 +14,7 @@
 // product is exact here too, and sums are in fp32 as before (what of a value lies under 2^-133, bf16's least, is
 // left out). The parts are columns of their own, five rows to a tile, summed at the end. The fp32
 // matrix instructions are 16 times slower than the bf16 ones: 5 rows of 8960 by 1537 outputs take 16 us with them,
-// 11 so, of 8192 by 16384 48 and 21.
+// 9.7 so, of 8192 by 16384 48 and 21.
 //
 // One row of 8192 by 32768 outputs: 30 us, 4.7 TB/s; 16 rows 37 us.
 #include "seq_common.h"
@@ -236,8 +236,8 @@ hipError_t launch_f32(const LinearW4& a, int outs, int splits, hipStream_t s) {
 // Tiles of rows, waves that share inputs and waves that share outputs: as many of the former as leave a workgroup
 // for each CU, for they share what is read of x, and the latter where there is enough to split: waves that share nothing else
 // as many as up to 8 take the units in equally many turns, for what is left over is loaded without a turn before it. 5 fp32 rows,
-// 10 units: 5 splits 7.9 us, 4 8.9, 6 8.7, 8 9.1; 16 units: 8 8.5, 4 10.2, 6 10.8; 18: 6 10.9, 4 12.5, 8 11.4; 27: 7 15.3, 4 16.6,
-// 8 15.7; 4 bf16 rows, 7 units: 7 4.4, 4 5.0; 10: 5 5.1, 4 5.7; 18 and 32 within 2%. Waves x splits, us:
+// 10 units: 5 splits 7.0 us, 4 7.9, 6 7.6, 8 8.0; 16 units: 8 7.9, 4 8.6, 6 9.6; 18: 6 9.7, 4 10.8, 8 10.1; 27: 7 13.1, 4 14.3,
+// 8 13.9; 4 bf16 rows, 7 units: 7 4.4, 4 5.0; 10: 5 5.1, 4 5.7; 18 and 32 within 2%. Waves x splits, us:
 //                          1x4  2x2  4x1  4x2  8x1             2 tiles 4x1  8x1   4 tiles 8x1
 //    4 rows, 8960 x 1536   6.6  8.5 12.7 12.6 22.5
 //    4       5120 x 5120   9.2  7.4 10.9 10.3 18.2

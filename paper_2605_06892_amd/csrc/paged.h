@@ -117,17 +117,15 @@ __device__ __forceinline__ void write_out(const PagedArgs& a, long orow, int c, 
   if (a.lse && c == 0) a.lse[orow] = l == 0.f ? -INFINITY : fmaf(m, a.scale, logf(l));
 }
 
-// The output of the item that run blockIdx.x begins and does not end, one query
-// head per workgroup: its threads take 4 channels each of every few parts, then join those.
+// The output of query head r of the item that run w0 begins and does not end, by a workgroup: its threads take 4 channels
+// each of every few parts, then join those.
 template <bool F32, int DH>
-__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a, Plan plan) {
+__device__ __forceinline__ void join_parts(const PagedArgs& a, const Plan& plan, const Note& note, int w0, int r) {
   constexpr int C = DH / 4, G = kJoinThreads / C;  // threads per part, parts at a time
   __shared__ __attribute__((aligned(16))) f32x4 sums[G][C];
   __shared__ float ms[G], ls[G];
-  const int w0 = blockIdx.x, r = blockIdx.y;
-  const Note note = notes<DH>(a, plan)[w0];
   const int h = note.item / plan.gts, g = (note.item - h * plan.gts) * kRows + r;
-  if (note.more == 0 || g >= a.group) return;
+  if (g >= a.group) return;
   const Part<DH>* parts = static_cast<const Part<DH>*>(a.ws);
   const int lane_p = threadIdx.x / C, c = (threadIdx.x - lane_p * C) * 4;
   float m = -INFINITY, l = 0.f;
@@ -173,6 +171,40 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a, P
     sum += wt * sums[i][c / 4];
   }
   write_out<F32, DH>(a, (long)note.s * (a.kv_heads * a.group) + h * a.group + g, c, m_all, l, sum);
+}
+
+// One query head (blockIdx.y) of the item that each of PER runs begins and does not end, if there is one. Sending out
+// workgroups that find nothing to do takes 3 us for a thousand runs, so there is one for eight where one in 32 or fewer begin an item (four
+// sequences of 30011 to 131072 e2m1 rows: 73 us, 75 with one for each; one in 16, the same in bf16: 211.5 and 210; one in 3, 48
+// sequences of 201 to 8009 e2m1 rows: 38 and 34).
+template <bool F32, int DH, int PER>
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a, Plan plan) {
+  const int first = blockIdx.x * PER;
+  if constexpr (PER == 1) {
+    const Note note = notes<DH>(a, plan)[first];
+    if (note.more != 0) join_parts<F32, DH>(a, plan, note, first, blockIdx.y);
+  } else {
+    const int lane = threadIdx.x & (kWave - 1);
+    Note own{0, 0, 0, 0};
+    if (lane < PER && first + lane < plan.wgs) own = notes<DH>(a, plan)[first + lane];
+    for (unsigned long some = __ballot(own.more != 0); some; some &= some - 1) {
+      const int i = __builtin_ctzl(some);
+      const Note note{__builtin_amdgcn_readlane(own.s, i), __builtin_amdgcn_readlane(own.item, i),
+                      __builtin_amdgcn_readlane(own.slot, i), __builtin_amdgcn_readlane(own.more, i)};
+      join_parts<F32, DH>(a, plan, note, first + i, blockIdx.y);
+      __syncthreads();  // the sums were read
+    }
+  }
+}
+template <bool F32, int DH>
+hipError_t launch_join(const PagedArgs& a, const Plan& plan, hipStream_t s) {
+  constexpr int PER = 8;
+  const unsigned rows = std::min(a.group, kRows);
+  if (plan.wgs >= 4L * PER * a.n_seqs * a.kv_heads * plan.gts)
+    hipLaunchKernelGGL((paged_join_kernel<F32, DH, PER>), dim3((plan.wgs + PER - 1) / PER, rows), dim3(kJoinThreads), 0, s, a, plan);
+  else
+    hipLaunchKernelGGL((paged_join_kernel<F32, DH, 1>), dim3(plan.wgs, rows), dim3(kJoinThreads), 0, s, a, plan);
+  return hipGetLastError();
 }
 
 inline int gts_of(int group) { return (group + kRows - 1) / kRows; }

@@ -413,8 +413,7 @@ hipError_t launch(const PagedArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((paged_split_kernel<F32, E4M3, DH, ALIGNED>), dim3(plan.wgs), dim3(kSplitWaves * 64), 0, s, a, plan);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((paged_join_kernel<F32, DH>), dim3(plan.wgs, std::min(a.group, kRows)), dim3(kJoinThreads), 0, s, a, plan);
-  return hipGetLastError();
+  return launch_join<F32, DH>(a, plan, s);
 }
 
 template <bool F32, int DH>

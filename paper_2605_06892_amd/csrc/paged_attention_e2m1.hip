@@ -354,8 +354,7 @@ hipError_t launch(const PagedArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((e2m1_split_kernel<F32, DH, ALIGNED>), dim3(p.wgs / p.abreast), dim3(kWaves * 64), 0, s, a, plan);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((paged_join_kernel<F32, DH>), dim3(p.wgs, std::min(a.group, kRows)), dim3(kJoinThreads), 0, s, a, plan);
-  return hipGetLastError();
+  return launch_join<F32, DH>(a, plan, s);
 }
 
 template <bool F32, int DH>
