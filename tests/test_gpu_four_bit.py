@@ -443,6 +443,27 @@ def test_paged_every_launch(dtype, lens, page, heads, kv, rows):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cache", ["e2m1", "e4m3", "own"])
+@pytest.mark.parametrize("heads", [1, 20])
+@pytest.mark.parametrize("lens", [[300, 40000, 250, 500], [0, 40000, 1], [257] * 4, [20000, 20001, 0, 0]], ids=range(4))
+def test_paged_few_items_of_many_runs(dtype, cache, heads, lens):
+    """Outputs joined eight runs to a workgroup, where several of the eight begin an item and where none does."""
+    dh, page = 64, 64
+    if cache == "e2m1":
+        q, k, v, held, table = paged_inputs4(11, dtype, lens, page, heads, 1, dh, max_pages=640)
+    else:
+        q, k, v, held, table = S.paged_inputs(11, dtype, dtype if cache == "own" else cache, lens, page, heads, 1, dh, max_pages=640)
+    nb = H.hsa_paged_attention_workspace_bytes(T[dtype], len(lens), heads, 1, dh, table.shape[1] * page)
+    o, ws = Guarded(q.shape, T[dtype], 1), Guarded((nb,), torch.uint8, 2)
+    ws.t.fill_(255)
+    _, lse = S.run_paged(q, held, table, lens, page, heads, 1, dh, 0.125, o.t, ws.t)
+    want, lw, A, Sm = S.paged_want(q, k, v, table, lens, page, k.shape[0] // page, heads, 1, dh, 0.125)
+    S.check(o.t, lse, want, lw, A, Sm, dtype, max(lens), dh)
+    o.check("o")
+    ws.check("workspace")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("max_pages", [0, 3, 300])
 def test_paged_without_rows(dtype, max_pages):
     """No pages in the table, and no pages in the cache: outputs of zeros."""
