@@ -225,10 +225,15 @@ hipError_t launch_bf16(const LinearW4& a, int outs, int splits, hipStream_t s) {
 template <int NT>
 hipError_t launch_f32(const LinearW4& a, int outs, int splits, hipStream_t s) {
   const int per = (std::min(a.rows, NT * 5) + outs - 1) / outs;
-  if (per <= 1) return launch<false, NT, 1>(a, outs, splits, s);
+  // as many as a launch below may ask for
+  if constexpr (NT < 4) {
+    if (per <= 1) return launch<false, NT, 1>(a, outs, splits, s);
+  }
   if (per <= 2) return launch<false, NT, 2>(a, outs, splits, s);
-  if (per <= 3) return launch<false, NT, 3>(a, outs, splits, s);
-  return launch<false, NT, 5>(a, outs, splits, s);
+  if constexpr (NT == 1) {
+    if (per > 3) return launch<false, NT, 5>(a, outs, splits, s);
+  }
+  return launch<false, NT, 3>(a, outs, splits, s);
 }
 
 }  // namespace
@@ -247,6 +252,18 @@ hipError_t launch_f32(const LinearW4& a, int outs, int splits, hipStream_t s) {
 //   32       8192 x 32768             63   63   58                   45     42       49
 //   64       5120 x 16384             37   36   33                   27     24       35
 //   64       8192 x 32768            112  112  102                   78     67       56
+// fp32 rows: cutting them is most of the work, so as many waves share x as leave the CUs filled. us:
+//                          1 tile 4x2  8x1        2 tiles 4x1  4x2  8x1   4 tiles 8x1
+//    5 rows, 8192 x 32768      38.5   35.9
+//    8       5120 x 5120       11.8   18.3              15.4  13.8 20.9        26.1
+//    8       8192 x 16384      35.6   29.0              26.1  24.4 30.6        39.4
+//   16       5120 x 5120       20.1   17.5              17.3  15.2 21.6        29.2
+//   16       5120 x 13824      39.8   31.8              25.3  27.7 23.2        29.7
+//   16       8192 x 16384      61.7   47.6              39.6  42.5 36.2        44.1
+//   16       8192 x 32768       123   97.9              77.6  84.1 74.4        53.0
+//   64       1536 x 8960       47.6   18.4              17.1  30.4 17.2        23.6
+//   64       5120 x 5120       46.5   39.3              35.4  39.4 40.3        33.2
+//   64       8192 x 16384       183    145               123   138  121         102
 hipError_t launch_linear_w4(const LinearW4& a, bool bf16, hipStream_t s) {
   if (a.rows <= 0 || a.d_out <= 0) return hipSuccess;
   const long outs = (a.d_out + kOuts - 1) / kOuts, cus = compute_units();
@@ -254,7 +271,15 @@ hipError_t launch_linear_w4(const LinearW4& a, bool bf16, hipStream_t s) {
   const bool many = outs >= 2 * cus, some = outs >= cus;
   const int four = units >= 8 ? 2 : 1, two = units >= 2 ? 2 : 1, turns = (units + 7) / 8, one = (units + turns - 1) / turns;  // splits beside 4, 2 and 1
   if (!bf16) {
-    if (a.rows > 10 && outs >= 4 * cus) return launch_f32<4>(a, 4, 1, s);
+    auto groups = [&](int rows, int waves) { return (a.rows + rows - 1) / rows * ((outs + waves - 1) / waves); };
+    auto full = [&](long n) { return (double)n / ((n + cus - 1) / cus * cus); };  // of the CUs, in as many turns as n need
+    if (a.rows > 10 && full(groups(20, 8)) >= 0.75) return launch_f32<4>(a, 8, 1, s);
+    if (a.rows > 5) {
+      if (full(groups(10, 8)) >= 0.6) return launch_f32<2>(a, 8, 1, s);
+      const long n = groups(10, 4);
+      if (n >= 0.6 * cus) return launch_f32<2>(a, 4, n >= 2 * cus ? 1 : four, s);
+    }
+    if (outs >= 8 * cus) return launch_f32<1>(a, 8, 1, s);
     if (many || (some && a.rows > 5)) return launch_f32<1>(a, 4, four, s);
     return some ? launch_f32<1>(a, 2, two, s) : launch_f32<1>(a, 1, one, s);
   }

@@ -221,6 +221,19 @@ def test_linear_every_split(dtype, rows, units, less):
     y.check("y")
 
 
+@pytest.mark.parametrize("rows,d_in,d_out", [
+    (16, 608, 24600), (20, 1120, 24600), (41, 96, 24600),     # four tiles of five rows, eight waves that share them
+    (6, 4640, 19700), (10, 608, 24600), (33, 544, 9900),      # two tiles, eight waves
+    (7, 4128, 9900), (10, 4640, 9900), (10, 544, 9900), (64, 1056, 4900),   # two tiles, four waves, their inputs split or not
+    (1, 544, 32800), (5, 1120, 32800), (5, 544, 8200), (8, 4640, 4200), (9, 544, 4200)])  # one tile
+def test_linear_every_f32_launch(rows, d_in, d_out):
+    x, codes, ex = linear_case(rows + d_out, "f32", rows, d_in, d_out)
+    y = Guarded((rows, d_out), torch.float32, 1)
+    H.hsa_linear_w4(x.to(DEV), rows, codes.to(DEV), ex.to(DEV), y.t)
+    linear_check(y.t, x, codes, ex, "f32")
+    y.check("y")
+
+
 @pytest.mark.parametrize("scale", [-100, -115, -126])
 def test_linear_small_f32_rows(scale):
     """fp32 rows are taken to within 2^-133 of each value: with values about 2^-115 that shows in an output of ordinary size."""
