@@ -215,11 +215,16 @@ hipError_t launch(const LinearW4& a, int outs, int splits, hipStream_t s) {
 template <int NT>
 hipError_t launch_bf16(const LinearW4& a, int outs, int splits, hipStream_t s) {
   const int per = (std::min(a.rows, NT * kOuts) + outs - 1) / outs;  // rows of x for each wave
-  if (per <= 1) return launch<true, NT, 1>(a, outs, splits, s);
-  if (per <= 2) return launch<true, NT, 2>(a, outs, splits, s);
-  if (per <= 4) return launch<true, NT, 4>(a, outs, splits, s);
-  if (NT > 1 || per <= 8) return launch<true, NT, 8>(a, outs, splits, s);
-  return launch<true, NT, 16>(a, outs, splits, s);
+  // as many as a launch below may ask for
+  if constexpr (NT == 1) {
+    if (per <= 1) return launch<true, NT, 1>(a, outs, splits, s);
+    if (per <= 2) return launch<true, NT, 2>(a, outs, splits, s);
+    if (per > 8) return launch<true, NT, 16>(a, outs, splits, s);
+  }
+  if constexpr (NT < 4) {
+    if (per <= 4) return launch<true, NT, 4>(a, outs, splits, s);
+  }
+  return launch<true, NT, 8>(a, outs, splits, s);
 }
 
 template <int NT>
@@ -252,6 +257,18 @@ hipError_t launch_f32(const LinearW4& a, int outs, int splits, hipStream_t s) {
 //   32       8192 x 32768             63   63   58                   45     42       49
 //   64       5120 x 16384             37   36   33                   27     24       35
 //   64       8192 x 32768            112  112  102                   78     67       56
+//                          2x2  4x1  4x2             2 tiles 4x2  4x1  8x1
+//    1 row,  8192 x 8192   10.4 15.1 14.0
+//   16       8192 x 8192   13.5 18.4 17.8
+//   16       2048 x 8192    5.6  5.9
+//   16       5120 x 10240  14.6 13.2 13.2                         13.8
+//   32       5120 x 5120   12.1 12.6 12.1                    15.8 16.6 23.7
+//   32       8192 x 8192   20.3 18.4 17.4                    21.9 23.6 33.4
+//   32       5120 x 10240  17.9 17.0 18.0                    16.2 16.9
+//   64       5120 x 5120   17.1 16.5 17.1                    15.7 16.6 22.9
+//   64       8192 x 8192   33.7 29.0 28.9                    22.7 24.4 32.4
+//   64       5120 x 10240  27.8 27.9 26.1                    27.3 23.3 23.4
+// (4x2 of two tiles fill a CU's LDS: good where one turn of them fills the CUs.)
 // fp32 rows: cutting them is most of the work, so as many waves share x as leave the CUs filled. us:
 //                          1 tile 4x2  8x1        2 tiles 4x1  4x2  8x1   4 tiles 8x1
 //    5 rows, 8192 x 32768      38.5   35.9
@@ -268,7 +285,7 @@ hipError_t launch_linear_w4(const LinearW4& a, bool bf16, hipStream_t s) {
   if (a.rows <= 0 || a.d_out <= 0) return hipSuccess;
   const long outs = (a.d_out + kOuts - 1) / kOuts, cus = compute_units();
   const int units = (a.d_in + kUnit - 1) / kUnit;
-  const bool many = outs >= 2 * cus, some = outs >= cus;
+  const bool some = outs >= cus;
   const int four = units >= 8 ? 2 : 1, two = units >= 2 ? 2 : 1, turns = (units + 7) / 8, one = (units + turns - 1) / turns;  // splits beside 4, 2 and 1
   if (!bf16) {
     auto groups = [&](int rows, int waves) { return (a.rows + rows - 1) / rows * ((outs + waves - 1) / waves); };
@@ -280,17 +297,19 @@ hipError_t launch_linear_w4(const LinearW4& a, bool bf16, hipStream_t s) {
       if (n >= 0.6 * cus) return launch_f32<2>(a, 4, n >= 2 * cus ? 1 : four, s);
     }
     if (outs >= 8 * cus) return launch_f32<1>(a, 8, 1, s);
-    if (many || (some && a.rows > 5)) return launch_f32<1>(a, 4, four, s);
+    if (outs >= 2 * cus || (some && a.rows > 5)) return launch_f32<1>(a, 4, four, s);
     return some ? launch_f32<1>(a, 2, two, s) : launch_f32<1>(a, 1, one, s);
   }
   if (a.rows > 16) {
-    if (many) {
+    const long n = (a.rows + 31) / 32 * ((outs + 3) / 4);
+    if (units >= 2 && n <= cus && n >= 0.6 * cus) return launch_bf16<2>(a, 4, 2, s);
+    if (outs >= 2 * cus && n > cus) {
       if (outs < 8 * cus) return launch_bf16<2>(a, a.rows <= 32 ? 4 : 8, 1, s);
       return a.rows <= 32 ? launch_bf16<2>(a, 8, 1, s) : launch_bf16<4>(a, 8, 1, s);
     }
-    return some ? launch_bf16<1>(a, 4, 1, s) : launch_bf16<1>(a, 2, two, s);
+    return some ? launch_bf16<1>(a, 4, n > cus ? 1 : four, s) : launch_bf16<1>(a, 2, two, s);
   }
-  if (many) return launch_bf16<1>(a, 4, four, s);
+  if (outs > 2 * cus && (units < 8 || outs >= 2.5 * cus)) return launch_bf16<1>(a, 4, four, s);
   return some ? launch_bf16<1>(a, 2, two, s) : launch_bf16<1>(a, 1, one, s);
 }
 

@@ -234,6 +234,18 @@ def test_linear_every_f32_launch(rows, d_in, d_out):
     y.check("y")
 
 
+@pytest.mark.parametrize("rows,d_in,d_out", [
+    (17, 544, 9900), (32, 1056, 9900), (33, 1120, 5300), (64, 4640, 5300),   # two tiles, four waves, their inputs split
+    (33, 480, 5300), (128, 544, 5300), (17, 4640, 4200), (40, 4640, 4200),   # one tile, four waves
+    (5, 4640, 10300), (16, 4128, 10300), (16, 1056, 8200), (16, 4640, 8200), (3, 4640, 8200), (1, 96, 8200)])
+def test_linear_every_bf16_launch(rows, d_in, d_out):
+    x, codes, ex = linear_case(rows + d_out, "bf16", rows, d_in, d_out)
+    y = Guarded((rows, d_out), torch.bfloat16, 1)
+    H.hsa_linear_w4(x.to(DEV), rows, codes.to(DEV), ex.to(DEV), y.t)
+    linear_check(y.t, x, codes, ex, "bf16")
+    y.check("y")
+
+
 @pytest.mark.parametrize("scale", [-100, -115, -126])
 def test_linear_small_f32_rows(scale):
     """fp32 rows are taken to within 2^-133 of each value: with values about 2^-115 that shows in an output of ordinary size."""
