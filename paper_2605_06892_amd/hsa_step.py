@@ -350,6 +350,8 @@ def hsa_row_rms_scale(x, n_rows: int, scale, eps: float = RMS_EPS, stream=None) 
     _dev(x, scale)
     if scale.dtype != torch.float32:
         raise TypeError("row scales are fp32")
+    if n_rows * x.shape[1] > x.numel() or n_rows > scale.numel():
+        raise ValueError("x and scale must hold n_rows rows")
     st = lib().hsa_row_rms_scale(_dtype(x), _ptr(x), n_rows, x.shape[1], eps, _ptr(scale), _stream(stream))
     _check("hsa_row_rms_scale", st)
 

@@ -172,8 +172,15 @@ class Layer4:
         """y = the layer's output for the tokens x of pool.plan's last step: exactly one for every sequence, in their
         order (fresh was 1 throughout; an ended sequence goes on with any token and is released when another
         takes its place), or with `prompts` any number, where sequences begin (they attend to themselves
-        only). y may be x."""
+        only). y may be x. ValueError, with nothing enqueued, for more tokens than the layer or the pool was made for,
+        a decoding step of another number of tokens, and a y of other sizes than x."""
         n = x.shape[0]
+        if n > min(len(self.scale), len(self.qkv), len(self.o), len(pool.pos)):
+            raise ValueError(f"the layer takes {len(self.scale)} tokens a step and the pool plans {len(pool.pos)}, got {n}")
+        if not prompts and n != len(pool.lens):
+            raise ValueError(f"a decoding step has one token for each of {len(pool.lens)} sequences, got {n}")
+        if y.shape != x.shape:
+            raise ValueError("y is as large as x")
         q_width, kv_width = self.heads * self.head_dim, self.kv_heads * self.head_dim
         qkv, o = self.qkv[:n], self.o[:n]
         H.hsa_row_rms_scale(x, n, self.scale)

@@ -8,6 +8,7 @@ import torch
 import test_gpu_four_bit as F
 import test_gpu_seq as S
 import test_gpu_serving as N
+from gpu_util import Guarded
 from paper_2605_06892_amd import hsa_step as H
 from paper_2605_06892_amd import paged
 
@@ -135,3 +136,27 @@ def test_sequences_come_and_go():
     assert pool.free_at.tolist()[1:] == [0, 0] and torch.all(pool.slots[:25] >= 0)
     used = [x for r in pool.page_table.tolist() for x in r if x >= 0]
     assert len(set(used)) == len(used) == 6 and set(first) <= set(used)
+
+
+def test_step_of_too_many_tokens():
+    """Refused before anything is enqueued: what lies behind the layer's row scales stays, and so do the caches."""
+    lay = layer(S._gen(3), "bf16", 128, 4, 2, 64, 4)
+    guarded = Guarded((4,), torch.float32, 5)
+    lay.scale = guarded.t
+    lay.scale.fill_(7)
+    c = paged.PagedCache.allocate(16, 8, 2, 64, torch.bfloat16, e2m1=True)
+    c.k.fill_(3)
+    pool = paged.PagePool.allocate(16, 8, 5, 3, 9)
+    pool.plan(i32([1] * 5))
+    for n, prompts in ((5, False), (9, True), (4, False)):
+        x = torch.ones(n, 128, dtype=torch.bfloat16, device=DEV)
+        with pytest.raises(ValueError):
+            lay.step(x, c, pool, None, x, prompts=prompts)
+        with pytest.raises(ValueError):
+            H.hsa_row_rms_scale(x, n + 1, torch.empty(n + 1, device=DEV))
+        if n > 4:
+            with pytest.raises(ValueError):
+                H.hsa_row_rms_scale(x, n, lay.scale)
+    torch.cuda.synchronize()
+    guarded.check("scale")
+    assert torch.all(lay.scale == 7) and torch.all(c.k == 3)
