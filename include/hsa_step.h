@@ -767,7 +767,8 @@ int hsa_qk_norm_rope(int dtype, const void* q, int64_t q_stride, const void* k, 
  *   kv_lens    int32 [n_seqs]: past + fresh, at most R
  *   page_table int32 [n_seqs, max_pages]: entry i of sequence s with ceil(past / page_size)
  *              <= i < ceil(kv_lens / page_size) becomes the next free page, or -1 when there is none
- *              left. Other entries are kept
+ *              left. Other entries are kept: a page that was lacking is not asked for again and does not
+ *              count in a later call's free_next[2], the later tokens in it have no row either
  *   pos        int32 [n_tokens]: position of the token in its sequence; -1 behind the last
  *   slots      int32 [n_tokens]: its cache row (hsa_cache_store's idx); -1 behind the last token, past
  *              R, in a page whose entry is negative, and for a row that does not fit int32

@@ -21,7 +21,7 @@ which hands pages out on the device:
     attend    prefill or decode
     project   hsa_linear_w4                      back, and the residual
 
-Buffers are allocated once with torch and owned by the caller; nothing here computes.
+Buffers are allocated once with torch and owned by the caller; nothing here computes, but for a count of lacking pages.
 """
 
 from __future__ import annotations
@@ -109,6 +109,11 @@ class PagePool:
     pos: torch.Tensor         # [n_tokens]: their positions
     slots: torch.Tensor       # [n_tokens]: and their cache rows; -1 behind the last
     page_size: int
+    lacked: torch.Tensor | None = None  # [1]: pages that were lacking in all steps since the caller last set it to 0
+
+    def __post_init__(self):
+        if self.lacked is None:
+            self.lacked = torch.zeros(1, dtype=torch.int32, device=self.free_at.device)
 
     @classmethod
     def allocate(cls, n_pages: int, page_size: int, n_seqs: int, max_pages: int, n_tokens: int, device="cuda") -> "PagePool":
@@ -121,20 +126,38 @@ class PagePool:
 
     def plan(self, fresh: torch.Tensor) -> None:
         """fresh[s] more tokens for every sequence: their pages, positions and rows, and the new lengths. A step that finds too
-        few pages says so in free_at[2]; its tokens without a page have slot -1."""
+        few pages says so in free_at[2], and `lacked` keeps count of them over the steps. A page that was lacking is not
+        asked for again: the tokens in it, the later steps' too, have slot -1 and are left out by attention, until `resume`."""
         H.hsa_page_plan(self.lens, fresh, self.page_size, self.page_table, self.free, self.free_at, self.cu, self.lens,
                         self.pos, self.slots, self.free_at)
+        self.lacked.add_(self.free_at[2:])
 
     def release(self, seq: int) -> None:
         """A finished sequence's pages go back to the ring, and its length to 0. Waits for the device."""
-        n = -(-int(self.lens[seq]) // self.page_size)
-        pages = self.page_table[seq, :n]
+        self._cut(seq, 0)
+
+    def resume(self, seq: int) -> int:
+        """A sequence that was lacking a page goes back to the rows before it: what pages it has behind them go back to the
+        ring. Returns how many of its last tokens are to be planned and computed again; 0 if it has all its pages. Waits
+        for the device."""
+        rows = int(self.lens[seq])
+        gone = (self.page_table[seq, :-(-rows // self.page_size)] < 0).nonzero()
+        if len(gone) == 0:
+            return 0
+        keep = int(gone[0]) * self.page_size
+        self._cut(seq, keep)
+        return rows - keep
+
+    def _cut(self, seq: int, rows: int) -> None:
+        """Length `rows`, a multiple of the page size, and what pages are behind it to the ring."""
+        first, n = rows // self.page_size, -(-int(self.lens[seq]) // self.page_size)
+        pages = self.page_table[seq, first:n]
         pages = pages[pages >= 0]
         at = int(self.free_at[0]) + int(self.free_at[1])
         self.free[(torch.arange(len(pages), device=pages.device) + at) % len(self.free)] = pages
         self.free_at[1] += len(pages)
-        self.page_table[seq, :n] = -1
-        self.lens[seq] = 0
+        self.page_table[seq, first:n] = -1
+        self.lens[seq] = rows
 
 
 @dataclass
@@ -172,8 +195,9 @@ class Layer4:
         """y = the layer's output for the tokens x of pool.plan's last step: exactly one for every sequence, in their
         order (fresh was 1 throughout; an ended sequence goes on with any token and is released when another
         takes its place), or with `prompts` any number, where sequences begin (they attend to themselves
-        only). y may be x. ValueError, with nothing enqueued, for more tokens than the layer or the pool was made for,
-        a decoding step of another number of tokens, and a y of other sizes than x."""
+        only). Rows of a page that was lacking are left out, the newest among them (`PagePool.resume`). y may be x.
+        ValueError, with nothing enqueued, for more tokens than the layer or the pool was made for, a decoding step of
+        another number of tokens, and a y of other sizes than x."""
         n = x.shape[0]
         if n > min(len(self.scale), len(self.qkv), len(self.o), len(pool.pos)):
             raise ValueError(f"the layer takes {len(self.scale)} tokens a step and the pool plans {len(pool.pos)}, got {n}")

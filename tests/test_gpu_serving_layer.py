@@ -160,3 +160,41 @@ def test_step_of_too_many_tokens():
     torch.cuda.synchronize()
     guarded.check("scale")
     assert torch.all(lay.scale == 7) and torch.all(c.k == 3)
+
+
+def test_a_page_that_was_lacking_is_reported_and_made_good():
+    """Run out, free another sequence's page, plan one more token into the page that was lacking."""
+    pool = paged.PagePool.allocate(2, 8, 2, 3, 8)
+    pool.plan(i32([4, 4]))
+    pool.plan(i32([4, 4]))
+    assert pool.lacked.tolist() == [0] and pool.free_at.tolist()[1:] == [0, 0]
+    pool.plan(i32([0, 1]))
+    assert pool.lacked.tolist() == [1] and pool.free_at.tolist()[1:] == [0, 1] and pool.slots[:1].tolist() == [-1]
+    pool.release(0)
+    pool.plan(i32([0, 1]))
+    assert pool.lacked.tolist() == [1] and pool.slots[:1].tolist() == [-1] and pool.lens.tolist() == [0, 10]
+    assert pool.resume(0) == 0 and pool.resume(1) == 2 and pool.lens.tolist() == [0, 8]
+    pool.lacked.zero_()
+    pool.plan(i32([0, 2]))
+    page = int(pool.page_table[1, 1])
+    assert page >= 0 and pool.slots[:2].tolist() == [page * 8, page * 8 + 1] and pool.pos[:2].tolist() == [8, 9]
+    assert pool.lacked.tolist() == [0] and pool.lens.tolist() == [0, 10] and pool.free_at.tolist()[1:] == [0, 0]
+
+
+def test_lacking_pages_are_counted_over_replayed_steps():
+    page, n, width, pages = 4, 5, 9, 22
+    pool, one = paged.PagePool.allocate(pages, page, n, width, n), i32([1] * n)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        pool.plan(one)
+    for i in range(30):
+        graph.replay()
+        if i % 7 == 0:
+            torch.cuda.synchronize()
+            assert pool.lacked.tolist() == [max(0, n * -(-(i + 1) // page) - pages)]
+    assert pool.lacked.tolist() == [n * -(-30 // page) - pages] and pool.free_at.tolist()[1] == 0
+    assert [pool.resume(s) for s in range(n)] == [30 - 4 * 5 if s < 2 else 30 - 4 * 4 for s in range(n)]
+    assert pool.lens.tolist() == [20, 20, 16, 16, 16]

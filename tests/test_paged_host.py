@@ -70,3 +70,21 @@ def test_row_scales_are_as_many_as_rows(monkeypatch, rows, scales, n):
     monkeypatch.setattr(H, "lib", Library)
     with pytest.raises(ValueError):
         H.hsa_row_rms_scale(torch.zeros(rows, 8), n, torch.zeros(scales))
+
+
+def test_a_sequence_resumes_before_the_page_that_was_lacking():
+    p = paged.PagePool.allocate(8, 16, 3, 5, 20, device="cpu")
+    # 70 rows whose second page was lacking and whose later pages were not, 20 rows that have theirs, none
+    p.page_table[0] = torch.tensor([6, -1, 2, 7, -1], dtype=torch.int32)
+    p.page_table[1, :2] = torch.tensor([0, 1], dtype=torch.int32)
+    p.lens[:] = torch.tensor([70, 20, 0])
+    p.free[:] = torch.tensor([3, 4, 5, 0, 0, 0, 0, 0])
+    p.free_at[:] = torch.tensor([0, 3, 2])
+    p.lacked[:] = 2
+    assert p.resume(1) == 0 and p.resume(2) == 0 and p.lens.tolist() == [70, 20, 0] and p.free_at.tolist() == [0, 3, 2]
+    assert p.resume(0) == 54  # rows 16 to 69
+    assert p.lens.tolist() == [16, 20, 0] and p.page_table[0].tolist() == [6, -1, -1, -1, -1]
+    assert p.free_at.tolist() == [0, 5, 2] and p.free[:5].tolist() == [3, 4, 5, 2, 7]
+    assert p.resume(0) == 0 and p.lacked.tolist() == [2]
+    p.page_table[1, :2], p.lens[1] = torch.tensor([-1, 1], dtype=torch.int32), 17  # from its first page on
+    assert p.resume(1) == 17 and p.lens[1] == 0 and p.free_at.tolist() == [0, 6, 2] and int(p.free[5]) == 1
