@@ -173,37 +173,65 @@ __device__ __forceinline__ void join_parts(const PagedArgs& a, const Plan& plan,
   write_out<F32, DH>(a, (long)note.s * (a.kv_heads * a.group) + h * a.group + g, c, m_all, l, sum);
 }
 
-// One query head (blockIdx.y) of the item that each of PER runs begins and does not end, if there is one. Sending out
-// workgroups that find nothing to do takes 3 us for a thousand runs, so there is one for eight where one in 32 or fewer begin an item (four
-// sequences of 30011 to 131072 e2m1 rows: 73 us, 75 with one for each; one in 16, the same in bf16: 211.5 and 210; one in 3, 48
-// sequences of 201 to 8009 e2m1 rows: 38 and 34).
-template <bool F32, int DH, int PER>
+// One query head (blockIdx.y) of an item that a run begins and does not end. FEW: blockIdx.x counts those items, and the run is
+// found by looking through all notes; else it is the run, and its workgroup may find nothing to do. Sending out workgroups for
+// nothing takes 1 to 3 us for 512 to 1024 runs, so they are counted where there are 32 runs to an item or more. Counted, one for
+// each run, and eight runs to a workgroup, which joins what they begin in turn, us:
+//                                                                      counted   each   eight
+//     4 sequences of 30011 to 131072 e2m1 rows, 40/8 heads               72.7    74.5   72.5
+//     2 of 131072 bf16 rows, 40/8                                         189     191    189
+//     16 of 65536 e4m3 rows, 16/1                                        49.4    56.5   50.0
+//     16 of 200 bf16 rows in a table of 131072, 16/1                     11.4    12.0   15.2
+//     2 of 200 bf16 rows in a table of 131072, 40/8                      10.5    11.0   13.9
+template <bool F32, int DH, bool FEW>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(PagedArgs a, Plan plan) {
-  const int first = blockIdx.x * PER;
-  if constexpr (PER == 1) {
-    const Note note = notes<DH>(a, plan)[first];
-    if (note.more != 0) join_parts<F32, DH>(a, plan, note, first, blockIdx.y);
+  if constexpr (!FEW) {
+    const Note note = notes<DH>(a, plan)[blockIdx.x];
+    if (note.more != 0) join_parts<F32, DH>(a, plan, note, blockIdx.x, blockIdx.y);
   } else {
-    const int lane = threadIdx.x & (kWave - 1);
-    Note own{0, 0, 0, 0};
-    if (lane < PER && first + lane < plan.wgs) own = notes<DH>(a, plan)[first + lane];
-    for (unsigned long some = __ballot(own.more != 0); some; some &= some - 1) {
-      const int i = __builtin_ctzl(some);
-      const Note note{__builtin_amdgcn_readlane(own.s, i), __builtin_amdgcn_readlane(own.item, i),
-                      __builtin_amdgcn_readlane(own.slot, i), __builtin_amdgcn_readlane(own.more, i)};
-      join_parts<F32, DH>(a, plan, note, first + i, blockIdx.y);
-      __syncthreads();  // the sums were read
+    constexpr int W = kJoinThreads / kWave, N = kMostRuns / kJoinThreads;  // a wave looks through N times 64 notes
+    __shared__ int begins[W], at;  // items that the runs of each wave begin; the run sought
+    __shared__ Note found;
+    const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, first = wave * (N * kWave) + lane;
+    Note own[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      own[i] = Note{0, 0, 0, 0};
+      if (first + i * kWave < plan.wgs) own[i] = notes<DH>(a, plan)[first + i * kWave];
     }
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) n += __builtin_popcountl(__ballot(own[i].more != 0));
+    if (lane == 0) begins[wave] = n;
+    if (threadIdx.x == 0) at = -1;
+    __syncthreads();
+    int rank = -(int)blockIdx.x;  // of the next item, from the one sought
+#pragma unroll
+    for (int w = 0; w < W; ++w) rank += w < wave ? begins[w] : 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const unsigned long some = __ballot(own[i].more != 0);
+      const int before = __builtin_amdgcn_mbcnt_hi((unsigned)(some >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)some, 0));
+      if (own[i].more != 0 && rank + before == 0) {
+        found = own[i];
+        at = first + i * kWave;
+      }
+      rank += __builtin_popcountl(some);
+    }
+    __syncthreads();
+    const int run = uniform(at);
+    const Note note{uniform(found.s), uniform(found.item), uniform(found.slot), uniform(found.more)};
+    if (run >= 0) join_parts<F32, DH>(a, plan, note, run, blockIdx.y);
   }
 }
 template <bool F32, int DH>
 hipError_t launch_join(const PagedArgs& a, const Plan& plan, hipStream_t s) {
-  constexpr int PER = 8;
   const unsigned rows = std::min(a.group, kRows);
-  if (plan.wgs >= 4L * PER * a.n_seqs * a.kv_heads * plan.gts)
-    hipLaunchKernelGGL((paged_join_kernel<F32, DH, PER>), dim3((plan.wgs + PER - 1) / PER, rows), dim3(kJoinThreads), 0, s, a, plan);
+  const long items = (long)a.n_seqs * a.kv_heads * plan.gts;
+  if (plan.wgs >= 32 * items)
+    hipLaunchKernelGGL((paged_join_kernel<F32, DH, true>), dim3((unsigned)items, rows), dim3(kJoinThreads), 0, s, a, plan);
   else
-    hipLaunchKernelGGL((paged_join_kernel<F32, DH, 1>), dim3(plan.wgs, rows), dim3(kJoinThreads), 0, s, a, plan);
+    hipLaunchKernelGGL((paged_join_kernel<F32, DH, false>), dim3(plan.wgs, rows), dim3(kJoinThreads), 0, s, a, plan);
   return hipGetLastError();
 }
 

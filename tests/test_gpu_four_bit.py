@@ -489,6 +489,28 @@ def test_paged_few_items_of_many_runs(dtype, cache, heads, lens):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cache", ["e2m1", "e4m3", "own"])
+@pytest.mark.parametrize("lens,group,kv", [
+    ([200] * 16, 16, 1), ([200, 199], 5, 8),   # all begin in the first runs, which have a tile each
+    ([1, 0, 129, 128, 127, 4000], 4, 2),
+    ([3000 + 131 * i for i in range(16)], 2, 1),  # a little further apart each
+    ([40960], 20, 1), ([130], 1, 1)], ids=range(6))
+def test_paged_short_sequences_in_wide_tables(dtype, cache, lens, group, kv):
+    """Joins of items that begin wherever short sequences leave them in a table of many runs."""
+    dh, page, heads = 64, 64, group * kv
+    make = S.paged_inputs if cache != "e2m1" else lambda g, d, c, *a, **k: paged_inputs4(g, d, *a, **k)
+    q, k, v, held, table = make(len(lens), dtype, dtype if cache == "own" else cache, lens, page, heads, kv, dh, max_pages=640)
+    nb = H.hsa_paged_attention_workspace_bytes(T[dtype], len(lens), heads, kv, dh, table.shape[1] * page)
+    o, ws = Guarded(q.shape, T[dtype], 1), Guarded((nb,), torch.uint8, 2)
+    ws.t.fill_(255)
+    _, lse = S.run_paged(q, held, table, lens, page, heads, kv, dh, 0.125, o.t, ws.t)
+    want, lw, A, Sm = S.paged_want(q, k, v, table, lens, page, k.shape[0] // page, heads, kv, dh, 0.125)
+    S.check(o.t, lse, want, lw, A, Sm, dtype, max(lens), dh)
+    o.check("o")
+    ws.check("workspace")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("max_pages", [0, 3, 300])
 def test_paged_without_rows(dtype, max_pages):
     """No pages in the table, and no pages in the cache: outputs of zeros."""
