@@ -328,6 +328,23 @@ def test_linear_row_by_row(dtype):
         assert torch.equal(y, z)
 
 
+@pytest.mark.parametrize("dtype,most", [("bf16", 16), ("f32", 5)])
+@pytest.mark.parametrize("d_in,d_out", [(2080, 300), (8960, 1537), (512, 17), (5120, 4128), (1536, 8960), (3168, 12288),
+                                        (2048, 32784)])  # tiles of outputs from two to eight times the CUs
+def test_linear_row_alone_and_among_others(dtype, most, d_in, d_out):
+    """Up to 16 bf16 or 5 fp32 rows the inputs are split by d_in and d_out alone, so a row's sums are taken in one order and
+    their bits are the same whatever stands beside it. (Larger calls may split otherwise.)"""
+    x, codes, ex = linear_case(d_in + d_out, dtype, most, d_in, d_out)
+    scale = torch.rand(most, generator=S._gen(1)).to(DEV)
+    x, codes, ex = x.to(DEV), codes.to(DEV), ex.to(DEV)
+    y = torch.empty(most, d_out, dtype=x.dtype, device=DEV)
+    H.hsa_linear_w4(x, most, codes, ex, y, row_scale=scale)
+    for first, n in [(i, 1) for i in range(most)] + [(0, 2), (1, 3), (most - 4, 4), (1, most - 1)]:
+        z = torch.empty(n, d_out, dtype=x.dtype, device=DEV)
+        H.hsa_linear_w4(x[first:first + n], n, codes, ex, z, row_scale=scale[first:first + n])
+        assert torch.equal(z, y[first:first + n]), (first, n)
+
+
 @pytest.mark.parametrize("d_in,d_out", [(16384, 270000)])
 def test_linear_offsets_past_32_bits(d_in, d_out):
     """Weights of more than 2^31 bytes: outputs at both ends and in the middle."""
