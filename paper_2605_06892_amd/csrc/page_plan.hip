@@ -76,7 +76,7 @@ struct Ring {
 };
 
 __global__ __launch_bounds__(kThreads) void page_plan_kernel(PagePlan a, FastDiv page, int* lens_out, int* next_out) {
-  __shared__ int begins[kChunk + 1], pasts[kChunk], news[kChunk];  // first token, rows before, first new page
+  __shared__ int begins[kChunk], pasts[kChunk], news[kChunk];  // first token, rows before, first new page
   __shared__ int waves[kThreads / kWave];
   const int most = a.n_tokens, rows_most = a.max_pages * a.page_size;
   const Ring ring(a);
@@ -116,7 +116,6 @@ __global__ __launch_bounds__(kThreads) void page_plan_kernel(PagePlan a, FastDiv
     const int pages_end = exclusive(need, pages, INT32_MAX / 2, waves);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) news[threadIdx.x * kPer + i] = need[i];
-    if (threadIdx.x == 0) begins[kChunk] = tokens_end;
     __syncthreads();
     int top = 1;  // the greatest power of two below the number of sequences
     while (top * 2 < n) top *= 2;
