@@ -243,8 +243,10 @@ hipError_t launch_f32(const LinearW4& a, int outs, int splits, hipStream_t s) {
 
 }  // namespace
 
-// Tiles of rows, waves that share inputs and waves that share outputs: as many of the former as leave a workgroup
-// for each CU, for they share what is read of x, and the latter where there is enough to split: waves that share nothing else
+// Tiles of rows, waves that share inputs and waves that share outputs: as many of the former as leave half of the CUs a workgroup
+// or more, for they share what is read of x (in one tile of bf16 rows 2 from one tile of outputs per CU on, 4 from two or two and a half
+// on; few outputs and more than 16 rows take 2 all the same), and the latter where there is enough to split. The limits lie between
+// the sizes below whose best shapes differ; where between them the shapes cross was not measured. Waves that share nothing else
 // as many as up to 8 take the units in equally many turns, for what is left over is loaded without a turn before it. 5 fp32 rows,
 // 10 units: 5 splits 7.0 us, 4 7.9, 6 7.6, 8 8.0; 16 units: 8 7.9, 4 8.6, 6 9.6; 18: 6 9.7, 4 10.8, 8 10.1; 27: 7 13.1, 4 14.3,
 // 8 13.9; 4 bf16 rows, 7 units: 7 4.4, 4 5.0; 10: 5 5.1, 4 5.7; 18 and 32 within 2%. Waves x splits, us:

@@ -244,7 +244,8 @@ inline int gts_of(int group) { return (group + kRows - 1) / kRows; }
 //    64          700      11.8 11.8    1000 15.7 12.6    1500 21.3 16.2
 //   128         1000      16.7 19.1    1250 19.4 19.3    2000 28.0 25.4
 //   256         1000      20.6 26.0    2000 35.7 38.3    4000 73.5 75.4
-// (64 channels and e4m3 cross within a third of these.)
+// (64 channels and e4m3 cross within a third of these. e2m1 rows cross further out: 64 items of 700 rows 7.9 13.2, 128 of 1000 9.2
+// 15.0, 256 of 2000 15.4 25.0, 512 of 2000 27.5 32.7. They are dealt from the same lengths on as the others.)
 constexpr long kLeastWhole = 768;
 inline long whole_len(long items) {
   const int cus = compute_units();
